@@ -249,6 +249,121 @@ via_status via_gemm_bf16(const void *X, const void *W, float *C, int32_t M, int3
 via_status via_dimr_cost(const float *q_logits, const float *p_logits, int32_t rows, int32_t vocab, int32_t ld,
                          float temperature, float alpha, float beta, float *cost, void *stream);
 
+/* ---- operators over a paged cache ----------------------------------------
+ * The library's page layout, for layers of the caller's own: a drafter head, a
+ * verifier whose heads are normalised, attention that reads chosen blocks of a
+ * long context.  A call works on one layer slot of a pool and on a batch of
+ * rows, the new tokens of n_seqs sequences:
+ *   pool       device, 16-byte aligned, the layout of via_kv_desc:
+ *              [n_slots][n_kv_heads][n_blocks][K|V][page] of `dtype`.  The pools
+ *              of a KV handle are such pools.
+ *   table      device [n_seqs][table_ld]: page of positions 16 j .. 16 j + 15.  An
+ *              entry outside [0, n_blocks) names no page: nothing is read or
+ *              written there, and its keys are seen by no row.
+ *   row_start  device [n_seqs + 1], ascending from 0: the rows of sequence s are
+ *              row_start[s] .. row_start[s + 1] - 1 of every row array.  Rows from
+ *              row_start[n_seqs] to `rows` (a padded batch) belong to no sequence:
+ *              nothing of them is read, and their outputs stay as they were.
+ *   kv_len     device [n_seqs]: cached positions of the sequence, its new rows
+ *              included.  Row r of its n rows is position kv_len - n + r (a
+ *              negative one is not cached and sees nothing).
+ *   rows, max_kv  host bounds of the rows and of kv_len; they size grids and
+ *              workspaces.  Positions at or past max_kv (or past the table, or
+ *              2^30) are left alone as if they had no page.
+ * The device arrays are read by the kernels and by nothing else, so a captured
+ * call follows them on replay.  A pool's pages that a call writes must be
+ * different ones for different positions.
+ *
+ * Every call is asynchronous on `stream`, which must belong to the device that
+ * is current and holds the arrays; it allocates nothing.  A workspace is the
+ * call's alone until it has finished: calls that may overlap, on two streams or
+ * in two captured graphs, take different ones.  rows == 0 or n_seqs == 0 is a
+ * no-op.  Row arrays (q, out, ...) are row-major of `dtype` with a row length
+ * in elements; they and their rows are 16-byte aligned (EINVAL).  n_heads is a
+ * multiple of n_kv_heads, query head h reading K/V head h / (n_heads /
+ * n_kv_heads).  head_dim is 64 or 128, at most 65535 sequences and
+ * 2^27 rows (EUNSUPPORTED). */
+typedef struct {
+  void *pool;
+  int32_t dtype, n_slots, n_blocks, n_kv_heads, head_dim;
+  const int32_t *table;
+  int32_t table_ld, n_seqs;
+  const int32_t *row_start, *kv_len;
+  int32_t rows, max_kv;
+} via_paged;
+
+/* Append the rows' keys and values to the cache, heads normalised and rotated
+ * on the way, and write the queries that go with them.
+ *   qkv     [rows][qkv_ld]: the fused projection's rows, n_heads query heads,
+ *           then the K heads, then the V heads
+ *   q_gain, k_gain  [head_dim] of dtype, nullable: with a gain every query (key)
+ *           head x becomes x g / sqrt(mean x^2 + eps) first (RMS norm per head)
+ *   pos     device [rows] or NULL: rotary position of each row; NULL: its cache
+ *           position.  The pair (i, i + head_dim/2) of a head turns by
+ *           pos theta^(-2 i / head_dim).
+ *   q_out   [rows][q_ld], written; may be qkv itself with q_ld == qkv_ld (the
+ *           queries in place)
+ * Norms and rotations are fp32 (angles fp64), rounded once.  A row without a
+ * page gets its query but caches nothing. */
+via_status via_paged_append(const via_paged *c, int32_t slot, const void *qkv, int32_t qkv_ld, int32_t n_heads,
+                            const int32_t *pos, const void *q_gain, const void *k_gain, float eps, float theta,
+                            void *q_out, int32_t q_ld, void *stream);
+
+/* Attention of the rows over their sequences' cache (their own keys included):
+ * out = softmax(scale q K^T) V over the keys a row sees, for one token a
+ * sequence up to whole prompts.
+ *   window    0, or a row sees only the last `window` positions up to its own
+ *   row_mask  NULL: a row sees every position up to its own.  Else device
+ *             [rows]: a row sees the positions before the batch's, and position
+ *             kv_len - n + o (o < min(n, VIA_MAX_TREE_ROWS)) iff bit o of its mask
+ *             is set (a token tree; give no window, EINVAL).
+ *   out       [rows][out_ld], written; a row that sees nothing gets zeros
+ *   lse       fp32 [rows][n_heads] or NULL: log of the sum of exp(scale q K^T), -inf
+ *             for a row that sees nothing
+ *   workspace device, 256-byte aligned, >= via_paged_attend_bytes (ENOMEM; may be
+ *             NULL where that is 0)
+ * scale > 0.  A key that a row does not see adds nothing to it, whatever its page
+ * holds.  Scores, softmax and sums are fp32. */
+size_t via_paged_attend_bytes(const via_paged *c, int32_t n_heads, int32_t window);
+via_status via_paged_attend(const via_paged *c, int32_t slot, const void *q, int32_t q_ld, int32_t n_heads, float scale,
+                            int32_t window, const uint64_t *row_mask, void *out, int32_t out_ld, float *lse,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
+/* Mean keys of the blocks that the batch's rows complete: means (device fp32
+ * [n_seqs][n_kv_heads][max_blocks][head_dim], 16-byte aligned) gets, for block b
+ * of `block` tokens (32, 64 or 128; EUNSUPPORTED) with (kv_len - n) / block <= b <
+ * kv_len / block and b < max_blocks, the mean of its cached keys.  Others, and
+ * blocks with an absent page, stay as they were.  Called after every append, it keeps the means of
+ * all whole blocks. */
+via_status via_paged_block_means(const via_paged *c, int32_t slot, int32_t block, float *means, int32_t max_blocks,
+                                 void *stream);
+
+/* Choose n_sel blocks for every row and K/V head, for via_paged_attend_blocks.
+ * A row at position p sees blocks 0 .. p / block.  The first n_first and the last
+ * n_last of these are chosen (n_last >= 1: the row's own block, whose mean is not
+ * there yet), then those with the largest (sum of the K/V head's queries) . mean key,
+ * equal ones in block order (NaN last).  Scores are fp64.
+ *   q      [rows][q_ld], the queries of via_paged_append
+ *   means  as via_paged_block_means keeps them; max_blocks must cover max_kv
+ *   sel    device [rows][n_kv_heads][n_sel], written: ascending blocks, then -1
+ *          where the row sees fewer
+ *   workspace device, 256-byte aligned, >= via_paged_select_bytes (ENOMEM)
+ * n_first + n_last <= n_sel.  The pool and the table are not read. */
+size_t via_paged_select_bytes(const via_paged *c, int32_t block);
+via_status via_paged_select(const via_paged *c, const void *q, int32_t q_ld, int32_t n_heads, const float *means,
+                            int32_t max_blocks, int32_t block, int32_t n_first, int32_t n_last, int32_t n_sel,
+                            int32_t *sel, void *workspace, size_t workspace_bytes, void *stream);
+
+/* via_paged_attend over chosen blocks: row r sees, under K/V head g, the
+ * positions up to its own of the blocks sel[r][g][0 .. n_sel) (device int32, any
+ * order; a block listed twice counts twice, an entry that is negative or past
+ * the row's own block is passed over).  The other arguments are
+ * via_paged_attend's. */
+size_t via_paged_attend_blocks_bytes(const via_paged *c, int32_t n_heads, int32_t block, int32_t n_sel);
+via_status via_paged_attend_blocks(const via_paged *c, int32_t slot, const void *q, int32_t q_ld, int32_t n_heads,
+                                   float scale, int32_t block, const int32_t *sel, int32_t n_sel, void *out,
+                                   int32_t out_ld, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- sizes -------------------------------------------------------------- */
 size_t via_pool_bytes(const via_model_desc *desc, int32_t n_layer_slots, int32_t n_blocks, int32_t block_size);
 /* The workspace also holds, per sequence id, a ring of VIA_STATE_ROWS fp32

@@ -1,0 +1,147 @@
+// The paged-cache operators (via_paged_*): arguments of their kernels, the
+// geometry both sides agree on, and the launch wrappers.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "common.h"
+
+namespace via {
+
+// Pages, sequences and rows of a call (via_paged), with the layer slot folded
+// into the pool's address.
+struct PagedRef {
+  void* pool;  // pages of the call's layer slot: [kv_head][block][K|V][page]
+  int n_blocks, KVH;
+  const int32_t* table;  // [n_seqs][table_ld]
+  int table_ld, n_seqs;
+  const int32_t* row_start;  // [n_seqs + 1]
+  const int32_t* kv_len;     // [n_seqs]
+  int rows;                  // rows of the row arrays
+  int cap;                   // cache positions a call looks at: min(max_kv, table_ld * kBlock)
+  int pages;                 // table entries that these are in
+};
+
+struct AppendArgs {
+  PagedRef c;
+  const void* qkv;
+  int qkv_ld, H, hd;
+  const int32_t* pos;  // nullable
+  const void *q_gain, *k_gain;  // nullable
+  float eps;
+  void* q_out;
+  int q_ld;
+  double turn[64];  // rotations per position of pair i, in whole turns: theta^(-2i/hd) / (2 pi)
+};
+
+// Queries of one work-group of the streaming attention kernel: (row, head of
+// the group) pairs, one column block of the matrix instruction.
+constexpr int kPagedQueries = 32;
+// Keys whose pages a work-group looks up at a time.
+constexpr int kPagedChunk = 4096;
+
+struct PagedAttnArgs {
+  PagedRef c;
+  const void* q;
+  int q_ld, H, hd;
+  float scale;
+  int window;               // 0: none
+  const uint64_t* row_mask;  // nullable
+  // listed blocks (null: every key): sel[row][kv_head][n_sel], blocks of `block` keys
+  const int32_t* sel;
+  int n_sel, block;
+  void* out;
+  int out_ld;
+  float* lse;  // nullable, [rows][H]
+  // keys of a split (of the listed keys, or from the tile's first visible key on) and
+  // the splits a launch has; one split writes the output itself
+  int span, n_splits;
+  int n_items;  // tiles a launch covers per K/V head
+  float* part_o;   // [n_splits][rows][H][hd]
+  float* part_ml;  // [n_splits][rows][H][2]: maximum (log2 units), sum
+};
+
+struct MeansArgs {
+  PagedRef c;
+  int hd, block;
+  float* means;  // [n_seqs][KVH][max_blocks][hd]
+  int max_blocks;
+  int per_seq;  // blocks a sequence can complete in one call
+};
+
+struct SelectArgs {
+  PagedRef c;
+  const void* q;
+  int q_ld, H, hd;
+  const float* means;
+  int max_blocks, block, n_first, n_last, n_sel;
+  int32_t* sel;      // [rows][KVH][n_sel]
+  uint64_t* scores;  // workspace [rows][KVH][nb]: sortable scores
+  int nb;            // blocks a row may see: min(max_blocks, ceil(cap / block))
+};
+
+void launch_paged_append(bool bf16, const AppendArgs& a, hipStream_t s);
+void launch_paged_attention(bool bf16, const PagedAttnArgs& a, hipStream_t s);
+void launch_paged_means(bool bf16, const MeansArgs& a, hipStream_t s);
+void launch_paged_select(bool bf16, const SelectArgs& a, hipStream_t s);
+
+#ifdef __HIPCC__
+// Rows [first, first + n) of sequence s.  Values that are not ascending row
+// numbers give empty or overlapping ranges, never rows outside the arrays.
+__device__ __forceinline__ void seq_rows(const PagedRef& c, int s, int& first, int& n) {
+  first = min(max(c.row_start[s], 0), c.rows);
+  n = min(max(c.row_start[s + 1], first), c.rows) - first;
+}
+
+__device__ __forceinline__ int seq_len(const PagedRef& c, int s) { return max(c.kv_len[s], 0); }
+
+// The sequence of row t (uniform over the wave): lanes look at 64 sequences at
+// a time.  -1: no sequence has it.
+__device__ __forceinline__ int seq_of_row(const PagedRef& c, int t) {
+  const int lane = threadIdx.x & 63;
+  for (int s0 = 0; s0 < c.n_seqs; s0 += 64) {
+    int first = 0, n = 0;
+    if (s0 + lane < c.n_seqs) seq_rows(c, s0 + lane, first, n);
+    const uint64_t m = __ballot(t >= first && t - first < n);
+    if (m) return s0 + __ffsll((unsigned long long)m) - 1;
+  }
+  return -1;
+}
+
+// Tile `item` (uniform over the wave) when sequence after sequence is cut into
+// tiles of `per` units, `units` units a row: its sequence and number there.
+// Returns false past the last tile.
+__device__ __forceinline__ bool tile_of_item(const PagedRef& c, int item, int units, int per, int& seq, int& tile) {
+  const int lane = threadIdx.x & 63;
+  for (int s0 = 0; s0 < c.n_seqs; s0 += 64) {
+    int first = 0, n = 0;
+    if (s0 + lane < c.n_seqs) seq_rows(c, s0 + lane, first, n);
+    const int tiles = (int)(((long long)n * units + per - 1) / per);
+    int end = tiles;  // tiles of this and the lower lanes' sequences
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(end, o, 64);
+      if (lane >= o) end += v;
+    }
+    const uint64_t m = __ballot(item < end);
+    if (m) {
+      const int l = __ffsll((unsigned long long)m) - 1;
+      seq = s0 + l;
+      tile = item - (__shfl(end, l, 64) - __shfl(tiles, l, 64));
+      return true;
+    }
+    item -= __shfl(end, 63, 64);
+  }
+  return false;
+}
+
+// Page of a sequence's positions 16 i .. 16 i + 15; -1 where the table names
+// none, which every kernel leaves alone.
+__device__ __forceinline__ int page_of(const PagedRef& c, int seq, int i) {
+  if (i < 0 || i >= c.pages) return -1;
+  const int p = c.table[(size_t)seq * c.table_ld + i];
+  return p >= 0 && p < c.n_blocks ? p : -1;
+}
+#endif
+
+}  // namespace via

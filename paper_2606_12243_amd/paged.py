@@ -1,0 +1,202 @@
+"""Operators over a paged cache (via_paged_*), for layers of the caller's own.
+
+``PagedCache`` describes pages of this library's layout (a pool of one's own, or
+one of a KV handle's, ``PagedCache.of_handle``) and the page table of the
+sequences; ``PagedBatch`` the rows of one step or prompt chunk.  For every layer
+a program appends the rows and attends::
+
+    q = batch.append(slot, qkv, n_heads, q_gain=gq, k_gain=gk)
+    out = batch.attend(slot, q)
+
+and, where contexts are long, keeps the mean key of every whole block and reads
+chosen blocks only::
+
+    batch.block_means(slot, means)
+    sel = batch.select_blocks(q, means, n_sel=32)
+    out = batch.attend_blocks(slot, q, sel)
+
+The page table, row starts and lengths stay on the device and are read by the
+kernels, so a captured HIP graph follows them from replay to replay.  Calls run on
+the current stream of the cache's device.  Rows behind the last sequence keep
+what the output held (an output the call allocates holds nothing there).
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+import torch
+
+from . import via
+
+_DTYPES = {torch.float32: via.DTYPE_F32, torch.bfloat16: via.DTYPE_BF16}
+
+
+def _expect(cond, what):
+    if not cond:
+        raise ValueError(what)
+
+
+class PagedCache:
+    """``pool``: contiguous device tensor [n_slots, n_kv_heads, n_blocks, 2, 16 * head_dim]
+    (or that many elements flat, with ``n_slots``), fp32 or bf16.  ``table``: int32 [n_seqs,
+    pages] on the same device, rows contiguous; entries outside the pool name no page."""
+
+    def __init__(self, pool, n_kv_heads, head_dim, table, n_slots=None):
+        _expect(pool.is_cuda and pool.is_contiguous(), "the pool must be a contiguous device tensor")
+        _expect(pool.dtype in _DTYPES, f"a pool of {pool.dtype} (float32 or bfloat16)")
+        _expect(n_kv_heads >= 1 and head_dim >= 1, "n_kv_heads and head_dim must be positive")
+        n_slots = n_slots if n_slots is not None else (pool.shape[0] if pool.dim() == 5 else 1)
+        per_block = n_slots * n_kv_heads * 2 * via.BLOCK * head_dim
+        _expect(n_slots >= 1 and pool.numel() % per_block == 0, "the pool holds no whole blocks of these sizes")
+        self.pool, self.n_kv_heads, self.head_dim, self.n_slots = pool, n_kv_heads, head_dim, n_slots
+        self.n_blocks = pool.numel() // per_block
+        if pool.dim() == 5:
+            _expect(tuple(pool.shape) == (n_slots, n_kv_heads, self.n_blocks, 2, via.BLOCK * head_dim),
+                    f"a pool of shape {tuple(pool.shape)}")
+        self.device, self.dtype = pool.device, pool.dtype
+        self.set_table(table)
+
+    def set_table(self, table):
+        """Another page table (batches made from now on read it)."""
+        _expect(table.dim() == 2 and table.dtype == torch.int32 and table.device == self.device,
+                "the table must be an int32 matrix on the pool's device")
+        _expect(table.stride(1) == 1 and table.stride(0) >= table.shape[1], "the table's rows must be contiguous")
+        self.table = table
+
+    @classmethod
+    def of_handle(cls, kv: via.KV, cache, seq_ids, pages=None):
+        """The full or slim cache of a KV handle, with the block tables its sequences have now
+        (``pages`` columns at least)."""
+        m = kv.model.desc
+        tables = [kv.seq_info(s, cache)[1] for s in seq_ids]
+        width = max([1, pages or 1] + [len(t) for t in tables])
+        host = torch.full((len(tables), width), -1, dtype=torch.int32)
+        for i, t in enumerate(tables):
+            host[i, :len(t)] = torch.tensor(t, dtype=torch.int32)
+        pool = kv.pool_view(cache)
+        return cls(pool, m["n_kv_heads"], m["head_dim"], host.to(pool.device))
+
+
+class PagedBatch:
+    """Rows of a batch: sequence s has rows row_start[s] .. row_start[s + 1] - 1 (device int32
+    [n_seqs + 1]) and kv_len[s] cached positions, those rows included (device int32 [n_seqs]).
+    ``rows`` and ``max_kv`` bound the rows and the lengths."""
+
+    def __init__(self, cache: PagedCache, row_start, kv_len, rows, max_kv):
+        n = cache.table.shape[0]
+        for t, shape in ((row_start, (n + 1,)), (kv_len, (n,))):
+            _expect(t.dtype == torch.int32 and t.device == cache.device and tuple(t.shape) == shape
+                    and t.is_contiguous(), f"row_start and kv_len must be int32 [{n + 1}] and [{n}] on the pool's device")
+        self.cache, self.row_start, self.kv_len, self.table = cache, row_start, kv_len, cache.table
+        # (a table that is part of a wider one: no more than its own columns)
+        self.rows, self.max_kv, self.n_seqs = int(rows), min(int(max_kv), self.table.shape[1] * via.BLOCK), n
+        self.c = via.Paged(cache.pool.data_ptr(), _DTYPES[cache.dtype], cache.n_slots, cache.n_blocks, cache.n_kv_heads,
+                           cache.head_dim, self.table.data_ptr(), max(1, self.table.stride(0)), n, row_start.data_ptr(),
+                           kv_len.data_ptr(), self.rows, self.max_kv)
+        self._c = C.byref(self.c)
+
+    # ---- arguments
+    def _call(self, f, *args):
+        dev = self.cache.device
+        if torch.cuda.current_device() == dev.index:
+            return via.check(f(self._c, *args, torch.cuda.current_stream(dev).cuda_stream))
+        with torch.cuda.device(dev):
+            return via.check(f(self._c, *args, torch.cuda.current_stream(dev).cuda_stream))
+
+    def _rows_of(self, t, heads, what):
+        """Address and row length of a [rows, heads, head_dim] (or [rows, heads * head_dim]) tensor."""
+        hd = self.cache.head_dim
+        _expect(t.dtype == self.cache.dtype and t.device == self.cache.device, f"{what} must be as the pool is")
+        whole = t.dim() == 2 and t.shape[1] == heads * hd and t.stride(1) == 1
+        split = (t.dim() == 3 and t.shape[1:] == (heads, hd) and t.stride(2) == 1 and (heads == 1 or t.stride(1) == hd))
+        _expect((whole or split) and t.shape[0] == self.rows,
+                f"{what} of shape {tuple(t.shape)}: {self.rows} rows of {heads} heads of {hd}, a row contiguous")
+        return t.data_ptr(), (t.stride(0) if self.rows > 1 else heads * hd)
+
+    def _heads_of(self, q):
+        hd = self.cache.head_dim
+        _expect(q.dim() in (2, 3) and q.shape[-1] % hd == 0, f"q of shape {tuple(q.shape)}")
+        return q.shape[1] if q.dim() == 3 else q.shape[1] // hd
+
+    def _vector(self, t, dtype, shape, what):
+        if t is None:
+            return None
+        _expect(t.dtype == dtype and t.device == self.cache.device and tuple(t.shape) == shape and t.is_contiguous(),
+                f"{what} must be contiguous {dtype} {list(shape)} on the pool's device")
+        return t.data_ptr()
+
+    def _workspace(self, nbytes):
+        # per call: two calls in flight (streams, captured graphs) never share one
+        return torch.empty(nbytes, dtype=torch.uint8, device=self.cache.device) if nbytes else None
+
+    # ---- operators
+    def append(self, slot, qkv, n_heads, pos=None, q_gain=None, k_gain=None, eps=1e-5, theta=10000.0, out=None):
+        """Cache the rows' keys and values, heads normalised (with gains) and rotated; returns the
+        queries [rows, n_heads, head_dim].  ``qkv`` [rows, (n_heads + 2 n_kv_heads) * head_dim];
+        ``pos`` int32 [rows]: rotary positions other than the cache's; ``out``: where the queries
+        go, qkv[:, :n_heads * head_dim] among others."""
+        hd = self.cache.head_dim
+        src, ld = self._rows_of(qkv, n_heads + 2 * self.cache.n_kv_heads, "qkv")
+        if out is None:
+            out = torch.empty((self.rows, n_heads, hd), dtype=qkv.dtype, device=qkv.device)
+        dst, out_ld = self._rows_of(out, n_heads, "out")
+        if dst == src:
+            out_ld = ld
+        self._call(via.via_paged_append, slot, src, ld, n_heads, self._vector(pos, torch.int32, (self.rows,), "pos"),
+                   self._vector(q_gain, self.cache.dtype, (hd,), "q_gain"),
+                   self._vector(k_gain, self.cache.dtype, (hd,), "k_gain"), eps, theta, dst, out_ld)
+        return out
+
+    def _attend(self, f, q, heads, out, return_lse, head_args, tail_args, nbytes):
+        src, ld = self._rows_of(q, heads, "q")
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        dst, out_ld = self._rows_of(out, heads, "out")
+        lse = torch.empty((self.rows, heads), dtype=torch.float32, device=q.device) if return_lse else None
+        ws = self._workspace(nbytes)
+        self._call(f, head_args[0], src, ld, heads, *head_args[1:], *tail_args, dst, out_ld,
+                   lse.data_ptr() if return_lse else None, ws.data_ptr() if nbytes else None, nbytes)
+        return (out, lse) if return_lse else out
+
+    def attend(self, slot, q, scale=None, window=0, row_mask=None, out=None, return_lse=False):
+        """Attention of the rows over their cached sequences: causal, the last ``window`` positions
+        (0: all), or with ``row_mask`` (int64 [rows], bit o: the batch's own position o) a token
+        tree.  ``scale`` defaults to head_dim ** -0.5."""
+        heads = self._heads_of(q)
+        mask = self._vector(row_mask, torch.int64, (self.rows,), "row_mask")
+        scale = self.cache.head_dim ** -0.5 if scale is None else scale
+        nbytes = via.via_paged_attend_bytes(self._c, heads, window)
+        return self._attend(via.via_paged_attend, q, heads, out, return_lse, (slot, scale), (window, mask), nbytes)
+
+    def block_means(self, slot, means, block=64):
+        """Mean keys of the blocks the rows complete, into ``means`` (fp32 [n_seqs, n_kv_heads,
+        blocks, head_dim]); returns it."""
+        n = means.shape[2] if means.dim() == 4 else 0
+        addr = self._vector(means, torch.float32, (self.n_seqs, self.cache.n_kv_heads, n, self.cache.head_dim), "means")
+        self._call(via.via_paged_block_means, slot, block, addr, n)
+        return means
+
+    def select_blocks(self, q, means, n_sel, block=64, n_first=1, n_last=2, out=None):
+        """The blocks each row reads: int32 [rows, n_kv_heads, n_sel], ascending, then -1."""
+        heads, kvh = self._heads_of(q), self.cache.n_kv_heads
+        src, ld = self._rows_of(q, heads, "q")
+        n = means.shape[2] if means.dim() == 4 else 0
+        addr = self._vector(means, torch.float32, (self.n_seqs, kvh, n, self.cache.head_dim), "means")
+        if out is None:
+            out = torch.empty((self.rows, kvh, n_sel), dtype=torch.int32, device=q.device)
+        dst = self._vector(out, torch.int32, (self.rows, kvh, n_sel), "out")
+        nbytes = via.via_paged_select_bytes(self._c, block)
+        ws = self._workspace(nbytes)
+        self._call(via.via_paged_select, src, ld, heads, addr, n, block, n_first, n_last, n_sel, dst,
+                   ws.data_ptr() if nbytes else None, nbytes)
+        return out
+
+    def attend_blocks(self, slot, q, sel, block=64, scale=None, out=None, return_lse=False):
+        """``attend`` over the blocks listed in ``sel`` (int32 [rows, n_kv_heads, n_sel])."""
+        heads = self._heads_of(q)
+        n_sel = sel.shape[2] if sel.dim() == 3 else 0
+        lists = self._vector(sel, torch.int32, (self.rows, self.cache.n_kv_heads, n_sel), "sel")
+        scale = self.cache.head_dim ** -0.5 if scale is None else scale
+        nbytes = via.via_paged_attend_blocks_bytes(self._c, heads, block, n_sel)
+        return self._attend(via.via_paged_attend_blocks, q, heads, out, return_lse, (slot, scale), (block, lists, n_sel),
+                            nbytes)

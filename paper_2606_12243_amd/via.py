@@ -89,6 +89,12 @@ class SamplingC(C.Structure):
     _fields_ = [("alpha", C.c_float), ("beta", C.c_float), ("draft_probs", P), ("uniforms", P)]
 
 
+class Paged(C.Structure):
+    _fields_ = [("pool", P), ("dtype", I32), ("n_slots", I32), ("n_blocks", I32), ("n_kv_heads", I32),
+                ("head_dim", I32), ("table", P), ("table_ld", I32), ("n_seqs", I32), ("row_start", P),
+                ("kv_len", P), ("rows", I32), ("max_kv", I32)]
+
+
 def _sig(name, res, *args):
     f = getattr(lib, name)
     f.restype = res
@@ -102,6 +108,18 @@ via_pack_gate_up = _sig("via_pack_gate_up", I32, P, P, I32, I32, I32, P)
 via_gemm_bf16 = _sig("via_gemm_bf16", I32, P, P, P, I32, I32, I32, P)
 via_pool_bytes = _sig("via_pool_bytes", C.c_size_t, C.POINTER(ModelDesc), I32, I32, I32)
 via_dimr_cost = _sig("via_dimr_cost", I32, P, P, I32, I32, I32, C.c_float, C.c_float, C.c_float, P, P)
+via_paged_append = _sig("via_paged_append", I32, C.POINTER(Paged), I32, P, I32, I32, P, P, P, C.c_float, C.c_float, P,
+                        I32, P)
+via_paged_attend_bytes = _sig("via_paged_attend_bytes", C.c_size_t, C.POINTER(Paged), I32, I32)
+via_paged_attend = _sig("via_paged_attend", I32, C.POINTER(Paged), I32, P, I32, I32, C.c_float, I32, P, P, I32, P, P,
+                        C.c_size_t, P)
+via_paged_block_means = _sig("via_paged_block_means", I32, C.POINTER(Paged), I32, I32, P, I32, P)
+via_paged_select_bytes = _sig("via_paged_select_bytes", C.c_size_t, C.POINTER(Paged), I32)
+via_paged_select = _sig("via_paged_select", I32, C.POINTER(Paged), P, I32, I32, P, I32, I32, I32, I32, I32, P, P,
+                        C.c_size_t, P)
+via_paged_attend_blocks_bytes = _sig("via_paged_attend_blocks_bytes", C.c_size_t, C.POINTER(Paged), I32, I32, I32)
+via_paged_attend_blocks = _sig("via_paged_attend_blocks", I32, C.POINTER(Paged), I32, P, I32, I32, C.c_float, I32, P,
+                               I32, P, I32, P, P, C.c_size_t, P)
 via_workspace_bytes = _sig("via_workspace_bytes", C.c_size_t, C.POINTER(ModelDesc), I32, I32, I32, I32, I32)
 via_staging_bytes = _sig("via_staging_bytes", C.c_size_t, C.POINTER(ModelDesc), I32, I32, I32, I32)
 via_model_create = _sig("via_model_create", I32, C.POINTER(ModelDesc), C.POINTER(Weights), C.POINTER(P))
@@ -137,7 +155,10 @@ via_kv_timer_read = _sig("via_kv_timer_read", I32, P, I32, PI32, C.POINTER(C.c_d
 via_last_error = _sig("via_last_error", C.c_char_p)
 via_version = _sig("via_version", C.c_char_p)
 
-EXPORTS = ["via_packed_bytes", "via_pack_weight", "via_pack_gate_up", "via_gemm_bf16", "via_dimr_cost", "via_pool_bytes", "via_workspace_bytes", "via_staging_bytes", "via_model_create",
+EXPORTS = ["via_packed_bytes", "via_pack_weight", "via_pack_gate_up", "via_gemm_bf16", "via_dimr_cost", "via_paged_append",
+           "via_paged_attend_bytes", "via_paged_attend", "via_paged_block_means", "via_paged_select_bytes",
+           "via_paged_select", "via_paged_attend_blocks_bytes", "via_paged_attend_blocks",
+           "via_pool_bytes", "via_workspace_bytes", "via_staging_bytes", "via_model_create",
            "via_model_set_route", "via_model_destroy", "via_kv_create", "via_kv_destroy",
            "via_kv_seq_reserve", "via_prefill", "via_prefill_batch", "via_kv_seq_release", "via_kv_seq_info",
            "via_kv_last_full_start",
