@@ -95,8 +95,11 @@ constexpr int kTargetGroups = 512;
 constexpr int kMinSpan = 128;
 struct Split {
   long long n_items;  // tiles a launch covers per K/V head
-  int span, n_splits;
+  int span, n_splits, tile_q;
 };
+// Rows times heads of a K/V head from which (on average over the sequences) a bf16 call
+// takes the kernel for many rows.
+constexpr int kManyQueries = 128;
 Split split_of(const via_paged* c, int n_heads, int window, int n_sel, int block) {
   Split s{};
   const int G = n_heads / c->n_kv_heads;
@@ -105,13 +108,15 @@ Split split_of(const via_paged* c, int n_heads, int window, int n_sel, int block
     const int per_row = ceil_div(G, kPagedQueries);
     tiles = s.n_items = (long long)c->rows * per_row;
     keys = (long long)n_sel * block;
+    s.tile_q = kPagedQueries;
   } else {
-    s.n_items = (long long)c->rows * G / kPagedQueries + c->n_seqs;
     const long long each = ((long long)c->rows + c->n_seqs - 1) / std::max(1, c->n_seqs);
-    tiles = (each * G + kPagedQueries - 1) / kPagedQueries * c->n_seqs;
+    s.tile_q = c->dtype == VIA_DTYPE_BF16 && each * G >= kManyQueries ? kPagedTileQueries : kPagedQueries;
+    s.n_items = (long long)c->rows * G / s.tile_q + c->n_seqs;
+    tiles = (each * G + s.tile_q - 1) / s.tile_q * c->n_seqs;
     keys = cap_of(c);
     // rows of a tile and the keys they look back on
-    if (window > 0) keys = std::min<long long>(keys, (long long)window + kPagedQueries / G + 32);
+    if (window > 0) keys = std::min<long long>(keys, (long long)window + s.tile_q / G + 32);
   }
   const long long groups = std::max<long long>(1, tiles * c->n_kv_heads);
   const long long want = std::min<long long>(std::max<long long>(1, kTargetGroups / groups), kMaxSplits);
@@ -139,6 +144,7 @@ via_status attention(const via_paged* c, int slot, PagedAttnArgs& a, void* works
   a.span = s.span;
   a.n_splits = s.n_splits;
   a.n_items = (int)s.n_items;
+  a.tile_q = s.tile_q;
   a.part_o = (float*)workspace;
   a.part_ml = (float*)workspace + (size_t)s.n_splits * c->rows * a.H * c->head_dim;
   launch_paged_attention(c->dtype == VIA_DTYPE_BF16, a, (hipStream_t)stream);

@@ -37,6 +37,8 @@ struct AppendArgs {
 // Queries of one work-group of the streaming attention kernel: (row, head of
 // the group) pairs, one column block of the matrix instruction.
 constexpr int kPagedQueries = 32;
+// ... and of the kernel for many rows.
+constexpr int kPagedTileQueries = 128;
 // Keys whose pages a work-group looks up at a time.
 constexpr int kPagedChunk = 4096;
 
@@ -57,6 +59,7 @@ struct PagedAttnArgs {
   // the splits a launch has; one split writes the output itself
   int span, n_splits;
   int n_items;  // tiles a launch covers per K/V head
+  int tile_q;   // queries of a tile: kPagedQueries or kPagedTileQueries
   float* part_o;   // [n_splits][rows][H][hd]
   float* part_ml;  // [n_splits][rows][H][2]: maximum (log2 units), sum
 };

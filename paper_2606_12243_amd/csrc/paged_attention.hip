@@ -162,19 +162,20 @@ __device__ __forceinline__ bool has_odd_values(const Block<T, HD>& b) {
   return m != 0;
 }
 // Takes them out of V.
+template <typename T>
+__device__ __forceinline__ uint32_t drop_odd(uint32_t w) {
+  const uint32_t m = odd_bits<T>(w);
+  return w & ~(sizeof(T) == 2 ? (m >> 15) * 0xFFFFu : (uint32_t)((int32_t)m >> 31));
+}
 template <typename T, int HD>
 __device__ __forceinline__ void drop_odd_values(Block<T, HD>& b) {
   using S = Shape<T, HD>;
-  auto drop = [](uint32_t w) {
-    const uint32_t m = odd_bits<T>(w);
-    return w & ~(sizeof(T) == 2 ? (m >> 15) * 0xFFFFu : (uint32_t)((int32_t)m >> 31));
-  };
 #pragma unroll
   for (int dt = 0; dt < S::DT; ++dt)
 #pragma unroll
     for (int n = 0; n < S::NV; ++n) {
       uint4& v = b.v[dt][n];
-      v = make_uint4(drop(v.x), drop(v.y), drop(v.z), drop(v.w));
+      v = make_uint4(drop_odd<T>(v.x), drop_odd<T>(v.y), drop_odd<T>(v.z), drop_odd<T>(v.w));
     }
 }
 // Bit i: the lane's query sees the key of score register i.
@@ -310,13 +311,32 @@ __device__ __forceinline__ void compute_block(Block<T, HD>& b, int kb, bool page
   }
 }
 
-// Tile t of a sequence's queries: the keys [lo, end) that its rows see, lo on a
-// page-pair border (dense: row r at position pos0 + r).
+// Queries q0 .. q0 + tile_q - 1 of a sequence: the keys [lo, end) that their rows
+// see, lo on a page-pair border.
 __device__ __forceinline__ void tile_keys(const PagedAttnArgs& a, int len, int n, int q0, int& lo, int& end) {
   const int G = a.H / a.c.KVH, pos0 = len - n;
-  const int r0 = q0 / G, r1 = min(n - 1, (q0 + kPagedQueries - 1) / G);
+  const int r0 = q0 / G, r1 = min(n - 1, (q0 + a.tile_q - 1) / G);
   end = min(a.row_mask ? len : pos0 + r1 + 1, a.c.cap);
   lo = a.window > 0 ? max(0, pos0 + r0 - a.window + 1) & ~31 : 0;
+}
+
+// Query qi = row * G + head of a sequence's queries under K/V head g.
+__device__ __forceinline__ Query query_of(const PagedAttnArgs& a, int g, int qi, int first, int n, int len) {
+  const int G = a.H / a.c.KVH, r = qi / G, pos = len - n + r;
+  Query q;
+  q.valid = r < n;
+  q.row = first + min(r, n - 1);
+  q.head = g * G + qi % G;
+  q.lo = a.window > 0 ? max(0, pos - a.window + 1) : 0;
+  q.vis = a.row_mask ? min(len - n, a.c.cap) : min(pos, a.c.cap - 1) + 1;
+  q.base = len - n;
+  q.mask = 0;
+  if (a.row_mask) {
+    // bits past the batch's own rows, or past the last key that a call looks at, are no keys
+    const int own = min(min(n, 64), max(a.c.cap - q.base, 0));
+    q.mask = (q.valid ? a.row_mask[q.row] : 0) & (own >= 64 ? ~0ull : (1ull << own) - 1);
+  }
+  return q;
 }
 
 template <typename T, int HD, bool LISTED>
@@ -359,24 +379,9 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void paged_stream_ke
     k0 = split * a.span;
     k1 = min(a.n_sel * a.block, k0 + a.span);
   } else {
-    const int q0 = tile * kPagedQueries, qi = q0 + ql, r = qi / G;
     int lo, end;
-    tile_keys(a, len, n, q0, lo, end);
-    q.valid = r < n;
-    q.row = first + min(r, n - 1);
-    q.head = g * G + qi % G;
-    const int pos = len - n + r;
-    q.lo = a.window > 0 ? max(0, pos - a.window + 1) : 0;
-    q.vis = a.row_mask ? min(len - n, a.c.cap) : min(pos, a.c.cap - 1) + 1;
-    q.base = len - n;
-    q.mask = a.row_mask && q.valid ? a.row_mask[q.row] : 0;
-    // bits of keys past the last one a call looks at are no keys
-    if (a.row_mask) {
-      const int room = a.c.cap - q.base;
-      q.mask &= room >= 64 ? ~0ull : room <= 0 ? 0ull : (1ull << room) - 1;
-      const int own = min(n, 64);
-      q.mask &= own >= 64 ? ~0ull : (1ull << own) - 1;
-    }
+    tile_keys(a, len, n, tile * kPagedQueries, lo, end);
+    q = query_of(a, g, tile * kPagedQueries + ql, first, n, len);
     k0 = lo + split * a.span;
     k1 = min(end, k0 + a.span);
     if (a.n_splits > 1 && k0 >= end) return;  // the joining kernel does not read it
@@ -519,6 +524,214 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void paged_stream_ke
   }
 }
 
+// ---------------------------------------------------------------------------
+// Many rows, bf16: the matrix instructions bound it.  A work-group takes 128
+// queries of one K/V head, a wave 32 of them; 64 keys at a time are copied into LDS
+// (asynchronously, the next 64 in flight) and read by all four waves as matrix
+// operands.  Pages are copied as they are, but that the two 16-byte halves of a V
+// row go apart, so that every operand read is 256 consecutive bytes per 16 lanes.
+// Two work-groups share a compute unit: one's softmax runs beside the other's
+// products.  P is rounded to one bf16 term here (to nearest; its error, 2^-9 of a
+// weight at most, is below the output's own rounding when a few keys share
+// the weight): two terms are half again the products.  The running maximum is
+// raised only when it grows by more than 2^8, which spares most rescalings of O;
+// weights up to 2^8 lose nothing.
+constexpr int kTileQueries = kPagedTileQueries, kTileKeys = 64;
+
+// 16 bytes a lane from base + voff to LDS at lds + 16 * lane (base, lds wave-uniform)
+__device__ __forceinline__ void lds_copy16(const void* base, uint32_t voff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base), "s"(lds) : "memory", "m0");
+}
+
+template <int HD>
+__global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
+  using S = Shape<uint16_t, HD>;
+  constexpr int DT = S::DT, NQ = S::NQ, kPage = kBlock * HD * 2;  // bytes of a K or V page
+  constexpr int kPieces = kPage / 1024;
+  __shared__ __align__(1024) unsigned char smem[2][2][4][kPage];  // [buffer][K, V][page]
+  const int G = a.H / a.c.KVH;
+  // blocks of a launch: K/V head fastest (with 8 of them an XCD keeps one head's pages in its L2), split, tile slowest
+  const int g = blockIdx.x % a.c.KVH, rest = blockIdx.x / a.c.KVH, split = rest % a.n_splits, item = rest / a.n_splits;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, ql = lane & 31, half = lane >> 5;
+  int seq, tile, first, n;
+  if (!tile_of_item(a.c, item, G, kTileQueries, seq, tile)) return;
+  seq_rows(a.c, seq, first, n);
+  if (tile < 0 || (long long)tile * kTileQueries >= (long long)n * G) return;
+  // the last rows, which see most keys, go first
+  tile = (int)(((long long)n * G + kTileQueries - 1) / kTileQueries) - 1 - tile;
+  const int len = seq_len(a.c, seq);
+  int lo, end;
+  tile_keys(a, len, n, tile * kTileQueries, lo, end);
+  const Query q = query_of(a, g, tile * kTileQueries + wave * 32 + ql, first, n, len);
+  const int k0 = lo + split * a.span, k1 = min(end, k0 + a.span);
+  if (a.n_splits > 1 && k0 >= end) return;  // the joining kernel does not read it
+  const int top = a.row_mask ? min(len, a.c.cap) : q.vis;  // the query sees no key from here on
+
+  uint4 qf[NQ];
+  {
+    const uint16_t* src = (const uint16_t*)a.q + (size_t)q.row * a.q_ld + (size_t)q.head * HD + half * 8;
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+      const uint4 v = *(const uint4*)(src + j * 16);
+      qf[j] = q.valid ? v : make_uint4(0, 0, 0, 0);
+    }
+  }
+  const float sl2 = a.scale * 1.4426950408889634f;
+  Acc<uint16_t, HD> acc;
+  acc.m = -INFINITY;
+  acc.l = 0.f;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc.o[dt][i] = 0.f;
+
+  const int tiles = k1 > k0 ? (k1 - k0 + kTileKeys - 1) / kTileKeys : 0;
+  const uint32_t lds = (uint32_t)(size_t)(__attribute__((address_space(3))) void*)&smem[0][0][0][0];
+  const uint32_t lds_w = __builtin_amdgcn_readfirstlane(lds + wave * kPage);
+  const uint32_t voff_k = lane * 16, voff_v = ((lane & 31) * 2 + half) * 16;
+  // lane i % 4 holds the page of tile t's keys 16 i .. 16 i + 15; wave w copies page w
+  auto pages_of = [&](int t) { return page_of(a.c, seq, (k0 >> 4) + t * 4 + (lane & 3)); };
+  auto copy = [&](int t, int pages) {
+    const int page = max(__builtin_amdgcn_readlane(pages, wave), 0);
+    const char* src = (const char*)a.c.pool + ((size_t)g * a.c.n_blocks + page) * 2 * kPage;
+    const uint32_t dst = lds_w + (t & 1) * 8 * kPage;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      lds_copy16(src + i * 1024, voff_k, dst + i * 1024);
+      lds_copy16(src + kPage + i * 1024, voff_v, dst + 4 * kPage + i * 1024);
+    }
+  };
+  const int key = ((ql >> 4) << 4) + (((ql >> 2) & 1) << 3) + (((ql >> 3) & 1) << 2) + (ql & 3);
+  const int k_at = (key >> 4) * kPage + half * 256 + (key & 15) * 16;
+
+  bool any_odd = false;
+  int pages = pages_of(0), pages1 = pages_of(1);
+  if (tiles > 0) copy(0, pages);
+  for (int t = 0; t < tiles; ++t) {
+    __builtin_amdgcn_s_waitcnt(0);  // the wave's copies have landed ...
+    __builtin_amdgcn_s_barrier();   // ... and all waves', and nobody reads the other buffer any more
+    const int pages2 = pages_of(t + 2);
+    if (t + 1 < tiles) copy(t + 1, pages1);
+    const int kb = k0 + t * kTileKeys;
+    const unsigned char* sk = &smem[t & 1][0][0][0];
+    const unsigned char* sv = &smem[t & 1][1][0][0];
+    if (__any(q.valid && kb < top && kb + kTileKeys > q.lo)) {
+      f32x16 s[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < NQ; ++j) s[b] = mma_bf16(*(const uint4*)(sk + k_at + b * 2 * kPage + j * 512), qf[j], s[b]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      const uint64_t absent = __ballot(pages < 0) & 15;
+      const bool whole = !absent && __all(!q.valid || (kb >= q.lo && kb + kTileKeys <= q.vis));
+      if (!whole) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const uint32_t seen = seen_keys<uint16_t>(q, kb + b * 32, !((absent >> (2 * b)) & 1), !((absent >> (2 * b + 1)) & 1), half);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[b][i] = (seen >> i) & 1 ? s[b][i] : -INFINITY;
+        }
+      }
+      float bm = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+      for (int i = 1; i < 16; ++i) bm = fmaxf(bm, fmaxf(s[0][i], s[1][i]));
+      bm = fmaxf(bm, __shfl_xor(bm, 32, 64));
+      const float mn = fmaxf(acc.m, bm * sl2);
+      if (__any(mn > acc.m + 8.f)) {  // (from -infinity: at the first key seen)
+        const float alpha = mn == acc.m ? 1.f : __builtin_amdgcn_exp2f(acc.m - mn);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) acc.o[dt] *= alpha;
+        acc.l *= alpha;
+        acc.m = mn;
+      }
+      const float neg_m = acc.m == -INFINITY ? 0.f : -acc.m;
+      uint4 p[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = (c & 1) * 8 + 2 * e;
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[c >> 1][i], sl2, neg_m));
+          const float p1 = __builtin_amdgcn_exp2f(fmaf(s[c >> 1][i + 1], sl2, neg_m));
+          acc.l += p0;
+          acc.l += p1;
+          const bf16x2 pk = {(__bf16)p0, (__bf16)p1};
+          w[e] = __builtin_bit_cast(uint32_t, pk);
+        }
+        p[c] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+      if (whole) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+            acc.o[dt] = mma_bf16(*(const uint4*)(sv + c * kPage + dt * 1024 + lane * 16), p[c], acc.o[dt]);
+      } else {
+        uint32_t bits = 0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) {
+            const uint4 v = *(const uint4*)(sv + c * kPage + dt * 1024 + lane * 16);
+            bits |= odd_bits<uint16_t>(v.x) | odd_bits<uint16_t>(v.y) | odd_bits<uint16_t>(v.z) | odd_bits<uint16_t>(v.w);
+            const uint4 u = make_uint4(drop_odd<uint16_t>(v.x), drop_odd<uint16_t>(v.y), drop_odd<uint16_t>(v.z),
+                                       drop_odd<uint16_t>(v.w));
+            acc.o[dt] = mma_bf16(u, p[c], acc.o[dt]);
+            __builtin_amdgcn_sched_barrier(0);  // (keeps few of them in registers)
+          }
+        any_odd |= __any(bits != 0);
+      }
+    }
+    pages = pages1;
+    pages1 = pages2;
+  }
+  if (any_odd) {  // (the same in all lanes)
+#pragma unroll 1
+    for (int t = 0; t < tiles; ++t) {
+      const int at = pages_of(t);
+      // every half of a tile that was not whole
+      const int kb = k0 + t * kTileKeys;
+      if (!(__ballot(at < 0) & 15) && __all(!q.valid || (kb >= q.lo && kb + kTileKeys <= q.vis))) continue;
+#pragma unroll 1
+      for (int b = 0; b < 2; ++b) {
+        const int page0 = __builtin_amdgcn_readlane(at, 2 * b), page1 = __builtin_amdgcn_readlane(at, 2 * b + 1);
+        add_odd_values<uint16_t, HD>(a.c, g, page0, page1, ql, half,
+                                     seen_keys<uint16_t>(q, kb + b * 32, page0 >= 0, page1 >= 0, half), acc);
+      }
+    }
+  }
+  if (!q.valid) return;
+  const float l = acc.l + __shfl_xor(acc.l, 32, 64);  // (a query's two lanes are both valid)
+  const bool direct = a.n_splits == 1;
+  const float inv = direct ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+  const size_t at = ((size_t)split * a.c.rows + q.row) * a.H + q.head;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4) {
+      const int d = dt * 32 + i4 * 8 + half * 4;
+      const f32x16& o = acc.o[dt];
+      const float x[4] = {o[i4 * 4] * inv, o[i4 * 4 + 1] * inv, o[i4 * 4 + 2] * inv, o[i4 * 4 + 3] * inv};
+      if (direct)
+        *(uint2*)((uint16_t*)a.out + (size_t)q.row * a.out_ld + (size_t)q.head * HD + d) =
+            make_uint2(pack_bf16x2(f2bf(x[0]), f2bf(x[1])), pack_bf16x2(f2bf(x[2]), f2bf(x[3])));
+      else
+        *(float4*)(a.part_o + at * HD + d) = make_float4(x[0], x[1], x[2], x[3]);
+    }
+  if (half == 0) {
+    if (!direct) {
+      a.part_ml[at * 2] = acc.m;
+      a.part_ml[at * 2 + 1] = l;
+    } else if (a.lse) {
+      a.lse[(size_t)q.row * a.H + q.head] = (acc.m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+    }
+  }
+}
+
 // Join the splits of each query in split order.  A work-group: one row, 1024 / HD
 // heads, HD / 8 threads each (8 dims a thread).
 template <typename T, int HD, bool LISTED>
@@ -533,7 +746,7 @@ __global__ __launch_bounds__(128) void paged_join_kernel(PagedAttnArgs a) {
     int first, n, lo, end;
     seq_rows(a.c, seq, first, n);
     const int G = a.H / a.c.KVH;
-    tile_keys(a, seq_len(a.c, seq), n, ((row - first) * G + head % G) / kPagedQueries * kPagedQueries, lo, end);
+    tile_keys(a, seq_len(a.c, seq), n, ((row - first) * G + head % G) / a.tile_q * a.tile_q, lo, end);
     splits = end > lo ? (int)min((long long)a.n_splits, ((long long)end - lo + a.span - 1) / a.span) : 0;
   }
   const size_t at = (size_t)row * a.H + head, step = (size_t)a.c.rows * a.H;
@@ -584,7 +797,14 @@ __global__ __launch_bounds__(128) void paged_join_kernel(PagedAttnArgs a) {
 template <typename T, int HD, bool LISTED>
 void launch(const PagedAttnArgs& a, hipStream_t s) {
   const int blocks = a.n_items * a.c.KVH * a.n_splits;
-  hipLaunchKernelGGL((paged_stream_kernel<T, HD, LISTED>), dim3(blocks), dim3(256), 0, s, a);
+  if constexpr (sizeof(T) == 2 && !LISTED) {
+    if (a.tile_q == kTileQueries)
+      hipLaunchKernelGGL(paged_tile_kernel<HD>, dim3(blocks), dim3(256), 0, s, a);
+    else
+      hipLaunchKernelGGL((paged_stream_kernel<T, HD, LISTED>), dim3(blocks), dim3(256), 0, s, a);
+  } else {
+    hipLaunchKernelGGL((paged_stream_kernel<T, HD, LISTED>), dim3(blocks), dim3(256), 0, s, a);
+  }
   if (a.n_splits > 1) {
     const int hpw = 128 / (HD / 8);
     hipLaunchKernelGGL((paged_join_kernel<T, HD, LISTED>), dim3(a.c.rows * ((a.H + hpw - 1) / hpw)), dim3(128), 0, s, a);

@@ -34,12 +34,19 @@ def say(*what):
     print("[case]", *what, flush=True)
 
 
+def weight_bits(b):
+    """bf16 calls of 128 queries a K/V head and sequence or more hold their weights as one bf16 value (to
+    nearest: 2^-8 of each at most), others as two (2^-15)."""
+    many = -(-b.T // len(b.rows)) * (b.H // b.KVH) >= 128
+    return 22 if b.dtype == F32 else 8 if many else 15
+
+
 def check_attention(b, q, got, lse, n, scale, p_bits=None, **kw):
     want, z, pv, amp = ref.attend(b, q, scale, **kw)
     live = torch.zeros(b.T, dtype=torch.bool)
     live[:b.start[-1]] = True
     tol, ztol = ref.bounds(b.dtype, b.hd, n, want, torch.nan_to_num(z, neginf=0.0), pv, amp,
-                           p_bits if p_bits else (15 if b.dtype == BF16 else 22))
+                           p_bits or (weight_bits(b) if kw.get("sel") is None else 22 if b.dtype == F32 else 15))
     err = (got.double().cpu() - want).abs()
     assert (err <= tol)[live].all(), float((err / tol)[live].max())
     zz = lse.double().cpu()
@@ -308,7 +315,7 @@ def test_layers_together():
             q = check_append(b, step, qkv, 10000.0, 1e-5, gains, None)
             b.pool = cache.pool.cpu()
             out, lse = step.attend(slot, q, return_lse=True)
-            check_attention(b, q.cpu(), out, lse, 420, hd ** -0.5, p_bits=8)
+            check_attention(b, q.cpu(), out, lse, 420, hd ** -0.5)
             before = means[slot].clone()
             step.block_means(slot, means[slot], block=32)
             torch.cuda.synchronize()
@@ -437,3 +444,57 @@ def test_more_than_32_bits_of_elements():
     for j, p in enumerate(far):
         w, m = want[0, :, int(b.table[0, j])], mag[0, :, int(b.table[0, j])]
         assert ((pool[0, :, p].double().cpu() - w).abs() <= 2.0 ** -8 * w.abs() * (m > 0) + 2.0 ** -19 * m).all()
+
+
+@pytest.mark.parametrize("H,KVH,hd", [(8, 2, 128), (4, 2, 64), (5, 5, 128), (32, 1, 64)])
+@pytest.mark.parametrize("rows,lens,kw", [
+    ([128, 131], [128, 1000], {}),             # prompt and chunk, whole and partial tiles
+    ([200, 0, 260], [100, 5, 330], {}),        # more rows than positions
+    ([300], [9000], {}),                       # split
+    ([150, 128], [700, 150], dict(window=70)),
+    ([130], [2000], dict(tree=True)),          # only its first 64 positions have bits
+])
+def test_attend_many_rows(H, KVH, hd, rows, lens, kw):
+    """The kernel for many rows."""
+    say("many rows", H, KVH, hd, rows, lens, kw)
+    b = ref.Batch(BF16, H, KVH, hd, rows, lens, seed=lens[0], pad=3)
+    q = (b.randn(b.T, H, hd) * 2).to(BF16)
+    masks = torch.randint(-2 ** 63, 2 ** 63 - 1, (b.T,), generator=b.g, dtype=torch.int64) if "tree" in kw else None
+    window = kw.get("window", 0)
+    out = torch.full((b.T, H, hd), 7.0, dtype=BF16, device="cuda")
+    _, lse = on_gpu(b).attend(b.slot, q.cuda(), window=window, row_mask=None if masks is None else masks.cuda(), out=out,
+                              return_lse=True)
+    torch.cuda.synchronize()
+    assert (out[b.start[-1]:] == 7).all()
+    assert weight_bits(b) == 8
+    check_attention(b, q, out, lse, b.max_kv, hd ** -0.5, window=window,
+                    masks=None if masks is None else masks.tolist())
+
+
+def test_values_no_row_may_see_many_rows():
+    say("unseen values, many rows")
+    H, KVH, hd = 8, 2, 128
+    b = ref.Batch(BF16, H, KVH, hd, [200], [333], seed=5)
+    b.table[0, 3] = -1
+    q = b.randn(b.T, H, hd).to(BF16)
+    clean = b.pool.clone()
+    v = b.pool[b.slot][:, :, 1].view(KVH, b.n_blocks, hd, 16)
+    for pos, dim, x in ((250, 9, math.nan), (251, 10, math.inf), (252, 127, -math.inf), (252, 64, math.inf), (253, 64, -math.inf)):
+        v[:, b.page(0, pos), dim, pos % 16] = x
+    last = b.page(0, 332)
+    v[:, last, :, 333 % 16:] = math.nan
+    b.pool[b.slot][:, :, 0].view(KVH, b.n_blocks, hd // 8, 16, 8)[:, last, :, 333 % 16:] = math.inf
+    out, lse = on_gpu(b).attend(b.slot, q.cuda(), return_lse=True)
+    torch.cuda.synchronize()
+    o = out.float().cpu()
+    first = 333 - 200  # row r is position first + r
+    for dim, pos, test in ((9, 250, torch.isnan), (10, 251, lambda t: t == math.inf), (127, 252, lambda t: t == -math.inf),
+                           (64, 253, torch.isnan)):
+        assert test(o[pos - first:, :, dim]).all()
+    assert (o[252 - first, :, 64] == math.inf).all()
+    b.pool = clean
+    want = ref.attend(b, q, hd ** -0.5)[0].to(BF16).cuda()
+    for dim, pos in ((9, 250), (10, 251), (127, 252), (64, 252)):
+        assert torch.isfinite(o[:pos - first, :, dim]).all()
+        out[pos - first:, :, dim] = want[pos - first:, :, dim]
+    check_attention(b, q, out, lse, b.max_kv, hd ** -0.5)
