@@ -203,22 +203,51 @@ __global__ __launch_bounds__(64) void paged_means_kernel(MeansArgs a) {
 // the last n_last of them are kept, and of the others the highest scores, ties
 // to the lower block, until n_sel are chosen.
 //
-// A work-group takes 16 rows of a sequence and one K/V head: its four waves score
-// 16 blocks at a time with v_mfma_f64_16x16x4_f64, and then choose for one row
-// after another.  A score is kept as 64 bits that order like it.
+// A work-group takes 16 rows of a sequence and one K/V head: its eight waves score
+// 16 blocks at a time with v_mfma_f64_16x16x4_f64, the next 16 blocks' means in
+// flight, and then choose for one row after another.  A score is kept as 64 bits
+// that order like it; a wave holds the upper halves of a row's scores in
+// registers and finds the n_sel-th largest bit by bit, which ends as soon as
+// n_sel of them are as large; lower halves are read only where upper ones tie.
+constexpr int kSelectThreads = 512, kSelectWaves = kSelectThreads / 64;
+constexpr int kSelectHeld = 32;  // scores a lane holds: rows of up to 64 * kSelectHeld blocks
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 
-// order of the doubles as unsigned numbers; NaN lowest but above 0
+// order of the doubles as unsigned numbers; NaN lowest, its upper half above 0
 __device__ __forceinline__ uint64_t sortable(double x) {
   const uint64_t u = (uint64_t)__double_as_longlong(x);
-  if (x != x) return 1;
+  if (x != x) return 1ull << 32;
   return u >> 63 ? ~u : u | 0x8000000000000000ull;
 }
 
-__device__ __forceinline__ int wave_count(bool p) { return __popcll(__ballot(p)); }
+// x[i] += the N values at p (16-byte aligned)
+template <typename T, int N>
+__device__ __forceinline__ void add_to(double (&x)[N], const T* p) {
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int i = 0; i < N; i += 8) {
+      const uint4 v = *(const uint4*)(p + i);
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[i + 2 * e] += (double)__uint_as_float(w[e] << 16);
+        x[i + 2 * e + 1] += (double)__uint_as_float(w[e] & 0xFFFF0000u);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const float4 v = *(const float4*)(p + i);
+      x[i] += (double)v.x;
+      x[i + 1] += (double)v.y;
+      x[i + 2] += (double)v.z;
+      x[i + 3] += (double)v.w;
+    }
+  }
+}
 
 template <typename T, int HD>
-__global__ __launch_bounds__(256) void paged_select_kernel(SelectArgs a) {
+__global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(SelectArgs a) {
   constexpr int KS = HD / 4;  // k steps; lane l holds dims (l/16) * KS .. + KS - 1 of row or block l % 16
   const int g = blockIdx.y, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, kq = lane >> 4;
   const int G = a.H / a.c.KVH;
@@ -231,27 +260,35 @@ __global__ __launch_bounds__(256) void paged_select_kernel(SelectArgs a) {
   const int rows = min(16, n - r0);
   // blocks the tile's last row sees (positions past the cap see what the last one does)
   const int seen = min(min(max(pos0 + rows - 1, -1), a.c.cap - 1) / a.block + 1, a.nb);
-  {
+  if (wave * 16 < seen) {
+    const float* means = a.means + ((size_t)seq * a.c.KVH + g) * (size_t)a.max_blocks * HD + kq * KS;
+    float4 v[KS / 4], u[KS / 4];
+    auto load = [&](float4 (&d)[KS / 4], int b0) {
+      const float* p = means + (size_t)min(b0 + m, seen - 1) * HD;
+#pragma unroll
+      for (int i = 0; i < KS / 4; ++i) d[i] = *(const float4*)(p + i * 4);
+    };
+    load(v, wave * 16);
     double q[KS];
 #pragma unroll
     for (int i = 0; i < KS; ++i) q[i] = 0.0;
     if (m < rows) {
       const T* p = (const T*)a.q + (size_t)(first + r0 + m) * a.q_ld + (size_t)g * G * HD + kq * KS;
-      for (int h = 0; h < G; ++h)
+      int h = 0;
+      for (; h + 4 <= G; h += 4) {  // (four heads' loads together)
 #pragma unroll
-        for (int i = 0; i < KS; ++i) q[i] += (double)to_f<T>(p[(size_t)h * HD + i]);
+        for (int i = 0; i < 4; ++i) add_to<T, KS>(q, p + (size_t)(h + i) * HD);
+      }
+      for (; h < G; ++h) add_to<T, KS>(q, p + (size_t)h * HD);
     }
-    const float* means = a.means + ((size_t)seq * a.c.KVH + g) * (size_t)a.max_blocks * HD + kq * KS;
-    for (int b0 = wave * 16; b0 < seen; b0 += 64) {
-      const float* p = means + (size_t)min(b0 + m, seen - 1) * HD;
+    auto score = [&](const float4 (&d)[KS / 4], int b0) {
       f64x4 s = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll
-      for (int i = 0; i < KS; i += 4) {
-        const float4 v = *(const float4*)(p + i);
-        s = __builtin_amdgcn_mfma_f64_16x16x4f64(q[i], (double)v.x, s, 0, 0, 0);
-        s = __builtin_amdgcn_mfma_f64_16x16x4f64(q[i + 1], (double)v.y, s, 0, 0, 0);
-        s = __builtin_amdgcn_mfma_f64_16x16x4f64(q[i + 2], (double)v.z, s, 0, 0, 0);
-        s = __builtin_amdgcn_mfma_f64_16x16x4f64(q[i + 3], (double)v.w, s, 0, 0, 0);
+      for (int i = 0; i < KS / 4; ++i) {
+        s = __builtin_amdgcn_mfma_f64_16x16x4f64(q[4 * i], (double)d[i].x, s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f64_16x16x4f64(q[4 * i + 1], (double)d[i].y, s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f64_16x16x4f64(q[4 * i + 2], (double)d[i].z, s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f64_16x16x4f64(q[4 * i + 3], (double)d[i].w, s, 0, 0, 0);
       }
       // register i of lane l: row 4 i + l / 16, block l % 16
 #pragma unroll
@@ -260,48 +297,85 @@ __global__ __launch_bounds__(256) void paged_select_kernel(SelectArgs a) {
         if (row < rows && b0 + m < seen)
           a.scores[((size_t)(first + r0 + row) * a.c.KVH + g) * a.nb + b0 + m] = sortable(s[i]);
       }
+    };
+    constexpr int kStep = kSelectWaves * 16;
+    for (int b0 = wave * 16; b0 < seen; b0 += 2 * kStep) {
+      load(u, b0 + kStep);
+      score(v, b0);
+      if (b0 + kStep >= seen) break;
+      load(v, b0 + 2 * kStep);
+      score(u, b0 + kStep);
     }
   }
   __syncthreads();
-  for (int r = wave; r < rows; r += 4) {
+  for (int r = wave; r < rows; r += kSelectWaves) {
     const int row = first + r0 + r, pos = min(pos0 + r, a.c.cap - 1);
     const int vis = pos < 0 ? 0 : min(pos / a.block + 1, a.nb);
     const uint64_t* sc = a.scores + ((size_t)row * a.c.KVH + g) * a.nb;
     int32_t* out = a.sel + ((size_t)row * a.c.KVH + g) * a.n_sel;
-    auto key = [&](int b) -> uint64_t {
-      if (b >= vis) return 0;
-      return b < a.n_first || b >= vis - a.n_last ? ~0ull : sc[b];
+    const int rounds = (vis + 63) >> 6;  // block of round j: 64 j + lane
+    auto kept = [&](int b) { return b < a.n_first || b >= vis - a.n_last; };
+    auto upper = [&](int b) -> uint32_t { return b >= vis ? 0u : kept(b) ? ~0u : (uint32_t)(sc[b] >> 32); };
+    auto lower = [&](int b) -> uint32_t { return kept(b) ? ~0u : (uint32_t)sc[b]; };
+    uint32_t held[kSelectHeld];
+#pragma unroll
+    for (int j = 0; j < kSelectHeld; ++j) held[j] = j < rounds ? upper(j * 64 + lane) : 0u;
+    // f(round, upper half) for every round
+    auto each = [&](auto f) {
+#pragma unroll
+      for (int j0 = 0; j0 < kSelectHeld; j0 += 4) {  // (past the last round they are 0)
+        if (j0 >= rounds) break;
+#pragma unroll
+        for (int j = j0; j < j0 + 4; ++j) f(j, held[j]);
+      }
+      for (int j = kSelectHeld; j < rounds; ++j) f(j, upper(j * 64 + lane));
     };
-    uint64_t at = 0;  // chosen: keys above `at`, and the first `ties` of those equal to it
+    // chosen: upper halves above hi; of those equal to it, lower halves above lo, and the first `ties` equal to that
+    uint32_t hi = 0, lo = ~0u;
     int ties = 0;
     if (vis > a.n_sel) {
-      // the n_sel-th largest key, bit by bit
       bool exact = false;
-      for (int bit = 63; bit >= 0 && !exact; --bit) {
-        const uint64_t t = at | (1ull << bit);
+      for (int bit = 31; bit >= 0 && !exact; --bit) {
+        const uint32_t t = hi | (1u << bit);
         int c = 0;
-        for (int b = lane; b - lane < vis; b += 64) c += wave_count(key(b) >= t);
-        if (c >= a.n_sel) at = t;
+        each([&](int, uint32_t k) { c += __popcll(__ballot(k >= t)); });
+        if (c >= a.n_sel) hi = t;
         exact = c == a.n_sel;
       }
       if (exact) {
-        at -= 1;
+        hi -= 1;
       } else {
         int above = 0;
-        for (int b = lane; b - lane < vis; b += 64) above += wave_count(key(b) > at);
-        ties = a.n_sel - above;
+        each([&](int, uint32_t k) { above += __popcll(__ballot(k > hi)); });
+        const int want = a.n_sel - above;
+        lo = 0;
+        for (int bit = 31; bit >= 0; --bit) {
+          const uint32_t t = lo | (1u << bit);
+          int c = 0;
+          each([&](int j, uint32_t k) { c += __popcll(__ballot(k == hi && lower(j * 64 + lane) >= t)); });
+          if (c >= want) lo = t;
+        }
+        above = 0;
+        each([&](int j, uint32_t k) { above += __popcll(__ballot(k == hi && lower(j * 64 + lane) > lo)); });
+        ties = want - above;
       }
     }
     int done = 0;
-    for (int b = lane; b - lane < vis; b += 64) {
-      const uint64_t k = key(b), lower = (1ull << lane) - 1;
-      const uint64_t tied = __ballot(k == at && b < vis);
-      bool take = b < vis && (k > at || (k == at && __popcll(tied & lower) < ties));
-      ties -= min(ties, __popcll(tied));
+    const uint64_t before = (1ull << lane) - 1;
+    each([&](int j, uint32_t k) {
+      const int b = j * 64 + lane;
+      bool take = b < vis && k > hi;
+      if (ties > 0 || lo != ~0u) {  // (uniform)
+        const uint32_t l = b < vis && k == hi ? lower(b) : 0u;
+        const bool eq = b < vis && k == hi;
+        const uint64_t tied = __ballot(eq && l == lo);
+        take |= eq && (l > lo || (l == lo && __popcll(tied & before) < ties));
+        ties -= min(ties, __popcll(tied));
+      }
       const uint64_t taken = __ballot(take);
-      if (take) out[done + __popcll(taken & lower)] = b;
+      if (take) out[done + __popcll(taken & before)] = b;
       done += __popcll(taken);
-    }
+    });
     for (int i = done + lane; i < a.n_sel; i += 64) out[i] = -1;
   }
 }
@@ -336,7 +410,7 @@ void launch_paged_means(bool bf16, const MeansArgs& a, hipStream_t s) {
 
 void launch_paged_select(bool bf16, const SelectArgs& a, hipStream_t s) {
   const dim3 grid((a.c.rows + 15) / 16 + a.c.n_seqs, a.c.KVH);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a); };
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kSelectThreads), 0, s, a); };
   if (bf16)
     a.hd == 128 ? go(paged_select_kernel<uint16_t, 128>) : go(paged_select_kernel<uint16_t, 64>);
   else

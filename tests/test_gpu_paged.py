@@ -498,3 +498,35 @@ def test_values_no_row_may_see_many_rows():
         assert torch.isfinite(o[:pos - first, :, dim]).all()
         out[pos - first:, :, dim] = want[pos - first:, :, dim]
     check_attention(b, q, out, lse, b.max_kv, hd ** -0.5)
+
+
+@pytest.mark.parametrize("len_,n_sel", [(32 * 2048, 40), (32 * 2049 + 5, 7), (32 * 3000, 100)])
+def test_select_of_many_blocks(len_, n_sel):
+    """Around the number of blocks whose scores a wave holds, with ties across it."""
+    say("select many", len_, n_sel)
+    b = ref.Batch(BF16, 2, 1, 64, [2], [16], seed=n_sel)
+    b.lens, b.max_kv = [len_], len_
+    b.kv_len = torch.tensor([len_], dtype=torch.int32)
+    b.table = torch.zeros((1, len_ // 16 + 1), dtype=torch.int32)
+    nb = -(-len_ // 32)
+    m = b.randn(1, 1, nb, 64)
+    m[0, 0, 100::500] = m[0, 0, 100].clone()
+    m[0, 0, 100::500, :2] += 3
+    q = b.randn(b.T, 2, 64).to(BF16)
+    q[:, :, :2] = 2
+    got = on_gpu(b).select_blocks(q.cuda(), m.cuda(), n_sel, block=32)
+    torch.cuda.synchronize()
+    assert torch.equal(got.cpu(), ref.select(b, q, m, n_sel, 32, 1, 2))
+
+
+def test_select_with_nan_scores_only():
+    say("select nan")
+    b = ref.Batch(BF16, 2, 1, 64, [3], [640], seed=1)
+    m = b.randn(1, 1, 20, 64)
+    m[:, :, 2:15] = math.nan
+    q = b.randn(b.T, 2, 64).to(BF16)
+    q[1] = math.nan
+    for n_sel in (4, 12, 18, 30):
+        got = on_gpu(b).select_blocks(q.cuda(), m.cuda(), n_sel, block=32)
+        torch.cuda.synchronize()
+        assert torch.equal(got.cpu(), ref.select(b, q, m, n_sel, 32, 1, 2)), n_sel
