@@ -130,12 +130,20 @@ __device__ __forceinline__ bool tile_of_item(const PagedRef& c, int item, int un
     if (m) {
       const int l = __ffsll((unsigned long long)m) - 1;
       seq = s0 + l;
-      tile = item - (__shfl(end, l, 64) - __shfl(tiles, l, 64));
+      tile = item - (__builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(tiles, l));
       return true;
     }
-    item -= __shfl(end, 63, 64);
+    item -= __builtin_amdgcn_readlane(end, 63);
   }
   return false;
+}
+
+// seq_rows and seq_len of a sequence that is the same in all lanes, as scalars.
+__device__ __forceinline__ void seq_of_wave(const PagedRef& c, int s, int& first, int& n, int& len) {
+  seq_rows(c, s, first, n);
+  first = __builtin_amdgcn_readfirstlane(first);
+  n = __builtin_amdgcn_readfirstlane(n);
+  len = __builtin_amdgcn_readfirstlane(seq_len(c, s));
 }
 
 // Page of a sequence's positions 16 i .. 16 i + 15; -1 where the table names

@@ -143,9 +143,9 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
 template <typename T, int HD>
 __global__ __launch_bounds__(64) void paged_means_kernel(MeansArgs a) {
   const int g = blockIdx.y, seq = blockIdx.z, lane = threadIdx.x;
-  int first, n;
-  seq_rows(a.c, seq, first, n);
-  const int len = min(seq_len(a.c, seq), a.c.cap), old = max(seq_len(a.c, seq) - n, 0);
+  int first, n, all;
+  seq_of_wave(a.c, seq, first, n, all);
+  const int len = min(all, a.c.cap), old = max(all - n, 0);
   const int b = old / a.block + blockIdx.x;
   if (b >= len / a.block || b >= a.max_blocks) return;
   float acc[HD / 32][8];
@@ -249,14 +249,15 @@ __device__ __forceinline__ void add_to(double (&x)[N], const T* p) {
 template <typename T, int HD>
 __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(SelectArgs a) {
   constexpr int KS = HD / 4;  // k steps; lane l holds dims (l/16) * KS .. + KS - 1 of row or block l % 16
-  const int g = blockIdx.y, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, kq = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int g = blockIdx.y, m = lane & 15, kq = lane >> 4;
   const int G = a.H / a.c.KVH;
-  int seq, tile, first, n;
+  int seq, tile, first, n, len;
   if (!tile_of_item(a.c, blockIdx.x, 1, 16, seq, tile)) return;
-  seq_rows(a.c, seq, first, n);
+  seq_of_wave(a.c, seq, first, n, len);
   const int r0 = tile * 16;
   if (tile < 0 || r0 >= n) return;
-  const int pos0 = seq_len(a.c, seq) - n + r0;  // position of the tile's first row
+  const int pos0 = len - n + r0;  // position of the tile's first row
   const int rows = min(16, n - r0);
   // blocks the tile's last row sees (positions past the cap see what the last one does)
   const int seen = min(min(max(pos0 + rows - 1, -1), a.c.cap - 1) / a.block + 1, a.nb);
@@ -315,11 +316,26 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(SelectArgs
     int32_t* out = a.sel + ((size_t)row * a.c.KVH + g) * a.n_sel;
     const int rounds = (vis + 63) >> 6;  // block of round j: 64 j + lane
     auto kept = [&](int b) { return b < a.n_first || b >= vis - a.n_last; };
-    auto upper = [&](int b) -> uint32_t { return b >= vis ? 0u : kept(b) ? ~0u : (uint32_t)(sc[b] >> 32); };
-    auto lower = [&](int b) -> uint32_t { return kept(b) ? ~0u : (uint32_t)sc[b]; };
+    auto read = [&](int b) { return sc[min(b, vis - 1)]; };
+    auto upper = [&](int b, uint64_t k) { return b >= vis ? 0u : kept(b) ? ~0u : (uint32_t)(k >> 32); };
+    auto lower = [&](int b) { return kept(b) ? ~0u : (uint32_t)read(b); };
     uint32_t held[kSelectHeld];
 #pragma unroll
-    for (int j = 0; j < kSelectHeld; ++j) held[j] = j < rounds ? upper(j * 64 + lane) : 0u;
+    for (int j0 = 0; j0 < kSelectHeld; j0 += 8) {
+      uint64_t k[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        held[j0 + j] = 0;
+        if (j0 < rounds) k[j] = read((j0 + j) * 64 + lane);  // (eight reads in flight)
+      }
+      if (j0 < rounds) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          held[j0 + j] = upper((j0 + j) * 64 + lane, k[j]);
+          __builtin_amdgcn_sched_barrier(0);  // (keeps the comparisons' masks few)
+        }
+      }
+    }
     // f(round, upper half) for every round
     auto each = [&](auto f) {
 #pragma unroll
@@ -328,7 +344,7 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(SelectArgs
 #pragma unroll
         for (int j = j0; j < j0 + 4; ++j) f(j, held[j]);
       }
-      for (int j = kSelectHeld; j < rounds; ++j) f(j, upper(j * 64 + lane));
+      for (int j = kSelectHeld; j < rounds; ++j) f(j, upper(j * 64 + lane, read(j * 64 + lane)));
     };
     // chosen: upper halves above hi; of those equal to it, lower halves above lo, and the first `ties` equal to that
     uint32_t hi = 0, lo = ~0u;
@@ -348,26 +364,26 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(SelectArgs
         int above = 0;
         each([&](int, uint32_t k) { above += __popcll(__ballot(k > hi)); });
         const int want = a.n_sel - above;
+        auto tied = [&](uint32_t t) {  // equal upper halves with lower ones >= t
+          int l = lane, c = 0;
+          asm volatile("" : "+v"(l));  // (recomputes the blocks: their masks would not fit the scalar registers)
+          each([&](int j, uint32_t k) { c += __popcll(__ballot(k == hi && lower(j * 64 + l) >= t)); });
+          return c;
+        };
         lo = 0;
-        for (int bit = 31; bit >= 0; --bit) {
-          const uint32_t t = lo | (1u << bit);
-          int c = 0;
-          each([&](int j, uint32_t k) { c += __popcll(__ballot(k == hi && lower(j * 64 + lane) >= t)); });
-          if (c >= want) lo = t;
-        }
-        above = 0;
-        each([&](int j, uint32_t k) { above += __popcll(__ballot(k == hi && lower(j * 64 + lane) > lo)); });
-        ties = want - above;
+        for (int bit = 31; bit >= 0; --bit)
+          if (tied(lo | (1u << bit)) >= want) lo |= 1u << bit;
+        ties = want - (lo == ~0u ? 0 : tied(lo + 1));
       }
     }
     int done = 0;
     const uint64_t before = (1ull << lane) - 1;
     each([&](int j, uint32_t k) {
       const int b = j * 64 + lane;
-      bool take = b < vis && k > hi;
+      bool take = k > hi;  // (0 where the row sees no block)
       if (ties > 0 || lo != ~0u) {  // (uniform)
-        const uint32_t l = b < vis && k == hi ? lower(b) : 0u;
-        const bool eq = b < vis && k == hi;
+        const bool eq = k == hi;
+        const uint32_t l = eq ? lower(b) : 0u;
         const uint64_t tied = __ballot(eq && l == lo);
         take |= eq && (l > lo || (l == lo && __popcll(tied & before) < ties));
         ties -= min(ties, __popcll(tied));

@@ -346,21 +346,18 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void paged_stream_ke
   const int G = a.H / a.c.KVH;
   // blocks of a launch: split fastest, K/V head, tile slowest
   const int split = blockIdx.x % a.n_splits, gi = blockIdx.x / a.n_splits, g = gi % a.c.KVH, item = gi / a.c.KVH;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, ql = lane & 31, half = lane >> 5;
-  int seq, tile, first, n;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, ql = lane & 31,
+            half = lane >> 5;
+  int seq, tile = 0, first, n, len;
   if constexpr (LISTED) {
     const int tiles = (G + kPagedQueries - 1) / kPagedQueries;  // tiles of a row's group
-    const int row = item / tiles;
-    seq = seq_of_row(a.c, row);
+    seq = seq_of_row(a.c, item / tiles);
     if (seq < 0) return;
-    seq_rows(a.c, seq, first, n);
-    tile = 0;
   } else {
     if (!tile_of_item(a.c, item, G, kPagedQueries, seq, tile)) return;
-    seq_rows(a.c, seq, first, n);
-    if (tile < 0 || (long long)tile * kPagedQueries >= (long long)n * G) return;
   }
-  const int len = seq_len(a.c, seq);
+  seq_of_wave(a.c, seq, first, n, len);
+  if (tile < 0 || (long long)tile * kPagedQueries >= (long long)n * G) return;
   Query q;
   int k0, k1;  // the work-group's keys: positions, or places in the row's list
   const int32_t* list = nullptr;
@@ -553,13 +550,12 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   // blocks of a launch: K/V head fastest (with 8 of them an XCD keeps one head's pages in its L2), split, tile slowest
   const int g = blockIdx.x % a.c.KVH, rest = blockIdx.x / a.c.KVH, split = rest % a.n_splits, item = rest / a.n_splits;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, ql = lane & 31, half = lane >> 5;
-  int seq, tile, first, n;
+  int seq, tile, first, n, len;
   if (!tile_of_item(a.c, item, G, kTileQueries, seq, tile)) return;
-  seq_rows(a.c, seq, first, n);
+  seq_of_wave(a.c, seq, first, n, len);
   if (tile < 0 || (long long)tile * kTileQueries >= (long long)n * G) return;
   // the last rows, which see most keys, go first
   tile = (int)(((long long)n * G + kTileQueries - 1) / kTileQueries) - 1 - tile;
-  const int len = seq_len(a.c, seq);
   int lo, end;
   tile_keys(a, len, n, tile * kTileQueries, lo, end);
   const Query q = query_of(a, g, tile * kTileQueries + wave * 32 + ql, first, n, len);
@@ -743,10 +739,10 @@ __global__ __launch_bounds__(128) void paged_join_kernel(PagedAttnArgs a) {
   if (seq < 0 || head >= a.H) return;
   int splits = a.n_splits;
   if constexpr (!LISTED) {
-    int first, n, lo, end;
-    seq_rows(a.c, seq, first, n);
+    int first, n, len, lo, end;
+    seq_of_wave(a.c, seq, first, n, len);
     const int G = a.H / a.c.KVH;
-    tile_keys(a, seq_len(a.c, seq), n, ((row - first) * G + head % G) / a.tile_q * a.tile_q, lo, end);
+    tile_keys(a, len, n, ((row - first) * G + head % G) / a.tile_q * a.tile_q, lo, end);
     splits = end > lo ? (int)min((long long)a.n_splits, ((long long)end - lo + a.span - 1) / a.span) : 0;
   }
   const size_t at = (size_t)row * a.H + head, step = (size_t)a.c.rows * a.H;
