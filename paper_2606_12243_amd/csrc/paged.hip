@@ -14,122 +14,183 @@ namespace {
 // where gains are given, then the pairs (i, i + hd/2) turned by pos theta^(-2i/hd);
 // v as it is.  Bound by memory: a value is read and written once.
 //
-// A work-group takes 16 consecutive rows and some of one K/V head's share of
-// them, its G query heads, its K and its V head.  Thread t holds 8 dims of row
-// t / 16 (16 lanes a row: a head of 128, or two of 64), so a head's sum of
+// A work-group takes the rows that enter one page of a sequence (at most 16) and
+// some of their heads, q, k and v in one list.  Thread t holds 8 dims of the page's
+// token t / 16 (16 lanes a token: a head of 128, or two of 64), so a head's sum of
 // squares and a dim's partner are lane exchanges, and q and k go out 16 bytes a
-// thread or more.  V, transposed in its pages, goes through LDS: 16 lanes write
-// 16 tokens of a dim next to each other.
+// thread or more.  V, transposed in its page, goes through LDS and out as 8 tokens
+// of a dim a thread, a whole page's in one piece.
 //
 // Angles are whole turns in fp64, pos * (theta^(-2i/hd) / 2 pi), of which only the
 // fraction is kept: fp32 would lose it at far positions (2^-24 of 10^5 turns).
 // Norms and rotations are fp32, rounded once where they are stored.
+__device__ __forceinline__ float ror8(float x) {  // from lane ^ 8 (of 16)
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x128, 0xF, 0xF, true));
+}
+// x of the lane's partner, half a head (TPH / 2 lanes) away
+template <int TPH>
+__device__ __forceinline__ float partner(float x) {
+  return TPH == 16 ? ror8(x) : __shfl_xor(x, TPH / 2, 64);
+}
+// sum over the TPH (8 or 16) lanes of a head: quad_perm exchanges 1 and 2 lanes
+// away, then the other quad (half mirror) and the other half (rotate by 8)
+template <int TPH>
+__device__ __forceinline__ float head_sum(float x) {
+  x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0xB1, 0xF, 0xF, true));
+  x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x4E, 0xF, 0xF, true));
+  x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x141, 0xF, 0xF, true));
+  return TPH == 16 ? x + ror8(x) : x;
+}
+
+// Page `item` (uniform) when the pages that each sequence's rows enter are counted
+// one sequence after another: its sequence and position / 16.  Positions
+// below 0 count as pages too (their rows only have queries).
+__device__ __forceinline__ bool page_of_item(const PagedRef& c, int item, int& seq, int& page) {
+  const int lane = threadIdx.x & 63;
+  for (int s0 = 0; s0 < c.n_seqs; s0 += 64) {
+    int first = 0, n = 0, len = 0;
+    if (s0 + lane < c.n_seqs) {
+      seq_rows(c, s0 + lane, first, n);
+      len = seq_len(c, s0 + lane);
+    }
+    const int p0 = (len - n) >> 4, pages = n > 0 ? ((len - 1) >> 4) - p0 + 1 : 0;
+    int end = pages;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(end, o, 64);
+      if (lane >= o) end += v;
+    }
+    const uint64_t m = __ballot(item < end);
+    if (m) {
+      const int l = __ffsll((unsigned long long)m) - 1;
+      seq = s0 + l;
+      page = __builtin_amdgcn_readlane(p0, l) + item - (__builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(pages, l));
+      return true;
+    }
+    item -= __builtin_amdgcn_readlane(end, 63);
+  }
+  return false;
+}
+
+// 8 values as floats, and back
+template <typename T>
+struct Eight {
+  uint4 v[sizeof(T) == 2 ? 1 : 2];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) v[i] = ((const uint4*)p)[i];
+  }
+  __device__ __forceinline__ void floats(float (&x)[8]) const {
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t w[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[2 * e] = __uint_as_float(w[e] << 16);
+        x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+      }
+    } else {
+      const uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(w[e]);
+    }
+  }
+};
+__device__ __forceinline__ void store8(uint16_t* p, const float (&y)[8]) {
+  *(uint4*)p = make_uint4(pack_bf16x2(f2bf(y[0]), f2bf(y[1])), pack_bf16x2(f2bf(y[2]), f2bf(y[3])),
+                          pack_bf16x2(f2bf(y[4]), f2bf(y[5])), pack_bf16x2(f2bf(y[6]), f2bf(y[7])));
+}
+__device__ __forceinline__ void store8(float* p, const float (&y)[8]) {
+  *(float4*)p = make_float4(y[0], y[1], y[2], y[3]);
+  *(float4*)(p + 4) = make_float4(y[4], y[5], y[6], y[7]);
+}
+
 template <typename T, int HD, bool NORM>
 __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
   constexpr int TPH = HD / 8, HPP = 16 / TPH, HALF = HD / 2;  // threads of a row per head; heads per pass
-  const int lane = threadIdx.x & 63, r = threadIdx.x >> 4, l = threadIdx.x & 15, sub = l / TPH, d0 = (l % TPH) * 8;
-  const int g = blockIdx.y, G = a.H / a.c.KVH;
-  const int row0 = blockIdx.x * 16, row = row0 + r;
-  __shared__ int s_seq[16], s_slot[16];
-  // sequences of the 16 rows: wave w finds rows 4 w .. 4 w + 3
-#pragma unroll 1
-  for (int i = 0; i < 4; ++i) {
-    const int m = (threadIdx.x >> 6) * 4 + i, t = row0 + m;
-    int seq = t < a.c.rows ? seq_of_row(a.c, t) : -1, slot = -1;
-    if (seq >= 0) {
-      int first, n;
-      seq_rows(a.c, seq, first, n);
-      slot = seq_len(a.c, seq) - n + (t - first);
-    }
-    if (lane == 0) {
-      s_seq[m] = seq;
-      s_slot[m] = slot;
-    }
-  }
-  __syncthreads();
-  const int seq = s_seq[r], slot = s_slot[r];
-  const bool live = seq >= 0;
-  const bool first = d0 < HALF;
-  float cs[8], sn[8];
+  constexpr int kVec = 16 / sizeof(T);                        // tokens of a dim a thread stores
+  constexpr int kStride = 16 + kVec;                          // of a dim in LDS (no bank conflicts on reading)
+  __shared__ __align__(16) T vt[HPP * HD * kStride];
+  const int l = threadIdx.x & 15, sub = l / TPH, d0 = (l % TPH) * 8, t = threadIdx.x >> 4;
+  int seq, page_no, first, n, len;
+  if (!page_of_item(a.c, blockIdx.x, seq, page_no)) return;
+  seq_of_wave(a.c, seq, first, n, len);
+  const int slot0 = page_no * 16, r = slot0 + t - (len - n);  // the thread's row of the sequence
+  const bool live = r >= 0 && r < n;
+  const int row = first + min(max(r, 0), n - 1);
+  const bool cached = slot0 >= 0 && slot0 + t < a.c.cap;
+  const int page = slot0 >= 0 ? __builtin_amdgcn_readfirstlane(page_of(a.c, seq, page_no)) : -1;
+  const int heads = a.H + 2 * a.c.KVH;
+  const T* src = (const T*)a.qkv + (size_t)row * a.qkv_ld + d0;
+  Eight<T> next;
+  const int step = gridDim.y * HPP;
+  int h0 = blockIdx.y * HPP;
+  next.load(src + (size_t)min(h0 + sub, heads - 1) * HD);
+  const bool low = d0 < HALF;
+  float cs[8], sn[8], qg[8], kg[8];
   {
-    const double pos = live ? (double)(a.pos ? a.pos[row] : slot) : 0.0;
+    const double pos = (double)(a.pos ? a.pos[row] : slot0 + t);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const double turns = pos * a.turn[d0 % HALF + e];
       const float f = (float)(turns - rint(turns));
       sincospif(2.f * f, &sn[e], &cs[e]);
+      if (low) sn[e] = -sn[e];
     }
   }
-  auto page_at = [&](int s, int p) { return s >= 0 && p >= 0 && p < a.c.cap ? page_of(a.c, s, p >> 4) : -1; };
-  const int page = page_at(seq, slot);
-  __shared__ float vt[HD][17];
-  // heads of this work-group: 0 .. G - 1 its queries, G the K head, G + 1 the V head
-  auto head = [&](int h) { return h < G ? g * G + h : h == G ? a.H + g : a.H + a.c.KVH + g; };
-  for (int h0 = blockIdx.z * HPP; h0 < G + 2; h0 += gridDim.z * HPP) {
-    const int h = h0 + sub;
-    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (live && h < G + 2) {
-      const T* p = (const T*)a.qkv + (size_t)row * a.qkv_ld + (size_t)head(h) * HD + d0;
-      if constexpr (sizeof(T) == 2) {
-        const uint4 v = *(const uint4*)p;
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[2 * e] = __uint_as_float(w[e] << 16);
-          x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = p[e];
-      }
-    }
-    float y[8];
-    if (NORM) {
-      float ss = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
-#pragma unroll
-      for (int o = 1; o < TPH; o <<= 1) ss += __shfl_xor(ss, o, 64);
-      const T* gain = (const T*)(h < G ? a.q_gain : h == G ? a.k_gain : nullptr);
-      const float sc = 1.0f / sqrtf(ss / (float)HD + a.eps);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = gain ? x[e] * sc * to_f<T>(gain[d0 + e]) : x[e];
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = x[e];
-    }
+  if (NORM) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float o = __shfl_xor(y[e], TPH / 2, 64);  // the pair's other half
-      const float t = first ? y[e] * cs[e] - o * sn[e] : y[e] * cs[e] + o * sn[e];
-      y[e] = h <= G ? t : y[e];
+      qg[e] = a.q_gain ? to_f<T>(((const T*)a.q_gain)[d0 + e]) : 0.f;
+      kg[e] = a.k_gain ? to_f<T>(((const T*)a.k_gain)[d0 + e]) : 0.f;
     }
-    T* dst = nullptr;
-    if (live && h < G)
-      dst = (T*)a.q_out + (size_t)row * a.q_ld + (size_t)head(h) * HD + d0;
-    else if (h == G && page >= 0)
-      dst = (T*)a.c.pool + k_off(0, page, a.c.n_blocks, a.c.KVH, HD, g, slot & 15, d0);
-    if (dst) {
-      if constexpr (sizeof(T) == 2) {
-        *(uint4*)dst = make_uint4(pack_bf16x2(f2bf(y[0]), f2bf(y[1])), pack_bf16x2(f2bf(y[2]), f2bf(y[3])),
-                                  pack_bf16x2(f2bf(y[4]), f2bf(y[5])), pack_bf16x2(f2bf(y[6]), f2bf(y[7])));
-      } else {
-        *(float4*)dst = make_float4(y[0], y[1], y[2], y[3]);
-        *(float4*)(dst + 4) = make_float4(y[4], y[5], y[6], y[7]);
-      }
-    }
-    if (h0 <= G + 1 && G + 1 < h0 + HPP) {  // uniform: this pass holds the V head
-      if (h == G + 1) {
+  }
+  for (; h0 < heads; h0 += step) {
+    const int h = h0 + sub;
+    float x[8];
+    next.floats(x);
+    if (h0 + step < heads) next.load(src + (size_t)min(h0 + step + sub, heads - 1) * HD);
+    if (h0 < a.H + a.c.KVH) {  // uniform: q or k heads
+      if (NORM) {
+        float ss = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) vt[d0 + e][r] = x[e];
+        for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
+        ss = head_sum<TPH>(ss);
+        const float sc = 1.0f / sqrtf(ss / (float)HD + a.eps);
+        const bool norm = h < a.H ? a.q_gain != nullptr : a.k_gain != nullptr && h < a.H + a.c.KVH;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = norm ? x[e] * sc * (h < a.H ? qg[e] : kg[e]) : x[e];
+      }
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = x[e] * cs[e] + partner<TPH>(x[e]) * sn[e];
+      if (live && h < a.H)
+        store8((T*)a.q_out + (size_t)row * a.q_ld + (size_t)h * HD + d0, y);
+      else if (live && cached && page >= 0 && h < a.H + a.c.KVH)
+        store8((T*)a.c.pool + k_off(0, page, a.c.n_blocks, a.c.KVH, HD, h - a.H, t, d0), y);
+    }
+    if (h0 + HPP > a.H + a.c.KVH) {  // uniform: v heads
+      const int g0 = h0 - a.H - a.c.KVH;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) vt[(sub * HD + d0 + e) * kStride + t] = from_f<T>(x[e]);
+      __syncthreads();
+      // tokens of the page that enter it
+      const int t0 = max(len - n - slot0, 0), t1 = min(min(len, a.c.cap) - slot0, 16);
+      if (page >= 0) {
+        for (int i = threadIdx.x; i < HPP * HD * 16 / kVec; i += 256) {
+          const int d = i * kVec / 16, at = i * kVec % 16, g = g0 + d / HD;
+          if (g < 0 || g >= a.c.KVH) continue;
+          const T* from = &vt[d * kStride + at];
+          T* to = (T*)a.c.pool + v_off(0, page, a.c.n_blocks, a.c.KVH, HD, g, at, d % HD);
+          if (t0 <= at && at + kVec <= t1) {
+            *(uint4*)to = *(const uint4*)from;
+          } else {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e)
+              if (at + e >= t0 && at + e < t1) to[e] = from[e];
+          }
+        }
       }
       __syncthreads();
-      // lane -> token threadIdx.x % 16, dims threadIdx.x / 16, + 16, ...
-      const int vr = threadIdx.x & 15, vslot = s_slot[vr], vpage = page_at(s_seq[vr], vslot);
-      if (vpage >= 0) {
-        T* vp = (T*)a.c.pool + v_off(0, vpage, a.c.n_blocks, a.c.KVH, HD, g, vslot & 15, 0);
-        for (int d = threadIdx.x >> 4; d < HD; d += 16) vp[(size_t)d * kBlock] = from_f<T>(vt[d][vr]);
-      }
     }
   }
 }
@@ -396,12 +457,14 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(SelectArgs
   }
 }
 
+constexpr int kAppendGroups = 2048;
+
 }  // namespace
 
 void launch_paged_append(bool bf16, const AppendArgs& a, hipStream_t s) {
-  // passes over heads go to further work-groups where the rows leave compute units idle
-  const int tiles = (a.c.rows + 15) / 16, heads = a.H / a.c.KVH + 2, passes = a.hd == 128 ? heads : (heads + 1) / 2;
-  const dim3 grid(tiles, a.c.KVH, std::min(passes, (512 + tiles * a.c.KVH - 1) / (tiles * a.c.KVH)));
+  // passes over heads go to further work-groups where the pages leave compute units idle
+  const int pages = a.c.rows / 16 + 2 * a.c.n_seqs, per_pass = 128 / a.hd, heads = a.H + 2 * a.c.KVH;
+  const dim3 grid(pages, std::min((heads + per_pass - 1) / per_pass, (kAppendGroups + pages - 1) / pages));
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a); };
   const bool norm = a.q_gain || a.k_gain;
   auto by = [&](auto k128, auto n128, auto k64, auto n64) {

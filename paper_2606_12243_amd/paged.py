@@ -94,40 +94,53 @@ class PagedBatch:
                            cache.head_dim, self.table.data_ptr(), max(1, self.table.stride(0)), n, row_start.data_ptr(),
                            kv_len.data_ptr(), self.rows, self.max_kv)
         self._c = C.byref(self.c)
+        self._sizes = {}  # workspace sizes by the arguments they depend on
 
     # ---- arguments
     def _call(self, f, *args):
         dev = self.cache.device
         if torch.cuda.current_device() == dev.index:
-            return via.check(f(self._c, *args, torch.cuda.current_stream(dev).cuda_stream))
-        with torch.cuda.device(dev):
-            return via.check(f(self._c, *args, torch.cuda.current_stream(dev).cuda_stream))
+            st = f(self._c, *args, torch.cuda.current_stream(dev).cuda_stream)
+        else:
+            with torch.cuda.device(dev):
+                st = f(self._c, *args, torch.cuda.current_stream(dev).cuda_stream)
+        if st != via.OK:
+            via.check(st)
 
     def _rows_of(self, t, heads, what):
         """Address and row length of a [rows, heads, head_dim] (or [rows, heads * head_dim]) tensor."""
-        hd = self.cache.head_dim
-        _expect(t.dtype == self.cache.dtype and t.device == self.cache.device, f"{what} must be as the pool is")
-        whole = t.dim() == 2 and t.shape[1] == heads * hd and t.stride(1) == 1
-        split = (t.dim() == 3 and t.shape[1:] == (heads, hd) and t.stride(2) == 1 and (heads == 1 or t.stride(1) == hd))
-        _expect((whole or split) and t.shape[0] == self.rows,
-                f"{what} of shape {tuple(t.shape)}: {self.rows} rows of {heads} heads of {hd}, a row contiguous")
-        return t.data_ptr(), (t.stride(0) if self.rows > 1 else heads * hd)
+        hd, shape, stride = self.cache.head_dim, t.shape, t.stride()
+        if t.dtype != self.cache.dtype or t.device != self.cache.device:
+            raise ValueError(f"{what} must be {self.cache.dtype} on {self.cache.device}, as the pool is")
+        if len(shape) == 3:
+            ok = shape[1] == heads and shape[2] == hd and stride[2] == 1 and (heads == 1 or stride[1] == hd)
+        else:
+            ok = len(shape) == 2 and shape[1] == heads * hd and stride[1] == 1
+        if not ok or shape[0] != self.rows:
+            raise ValueError(f"{what} of shape {tuple(shape)}: {self.rows} rows of {heads} heads of {hd}, a row contiguous")
+        return t.data_ptr(), (stride[0] if self.rows > 1 else heads * hd)
 
     def _heads_of(self, q):
         hd = self.cache.head_dim
-        _expect(q.dim() in (2, 3) and q.shape[-1] % hd == 0, f"q of shape {tuple(q.shape)}")
+        if q.dim() not in (2, 3) or q.shape[-1] % hd:
+            raise ValueError(f"q of shape {tuple(q.shape)}")
         return q.shape[1] if q.dim() == 3 else q.shape[1] // hd
 
     def _vector(self, t, dtype, shape, what):
         if t is None:
             return None
-        _expect(t.dtype == dtype and t.device == self.cache.device and tuple(t.shape) == shape and t.is_contiguous(),
-                f"{what} must be contiguous {dtype} {list(shape)} on the pool's device")
+        if t.dtype != dtype or t.device != self.cache.device or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{what} must be contiguous {dtype} {list(shape)} on {self.cache.device}")
         return t.data_ptr()
 
-    def _workspace(self, nbytes):
-        # per call: two calls in flight (streams, captured graphs) never share one
-        return torch.empty(nbytes, dtype=torch.uint8, device=self.cache.device) if nbytes else None
+    def _workspace(self, f, *args):
+        """A workspace (None if none is needed) and its size.  It is the call's own: two calls in flight
+        (streams, captured graphs) never share one."""
+        key = (f.__name__, args)
+        n = self._sizes.get(key)
+        if n is None:
+            n = self._sizes[key] = f(self._c, *args)
+        return (torch.empty(n, dtype=torch.uint8, device=self.cache.device) if n else None), n
 
     # ---- operators
     def append(self, slot, qkv, n_heads, pos=None, q_gain=None, k_gain=None, eps=1e-5, theta=10000.0, out=None):
@@ -147,13 +160,13 @@ class PagedBatch:
                    self._vector(k_gain, self.cache.dtype, (hd,), "k_gain"), eps, theta, dst, out_ld)
         return out
 
-    def _attend(self, f, q, heads, out, return_lse, head_args, tail_args, nbytes):
+    def _attend(self, f, q, heads, out, return_lse, head_args, tail_args, workspace):
         src, ld = self._rows_of(q, heads, "q")
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         dst, out_ld = self._rows_of(out, heads, "out")
         lse = torch.empty((self.rows, heads), dtype=torch.float32, device=q.device) if return_lse else None
-        ws = self._workspace(nbytes)
+        ws, nbytes = self._workspace(*workspace)
         self._call(f, head_args[0], src, ld, heads, *head_args[1:], *tail_args, dst, out_ld,
                    lse.data_ptr() if return_lse else None, ws.data_ptr() if nbytes else None, nbytes)
         return (out, lse) if return_lse else out
@@ -165,8 +178,8 @@ class PagedBatch:
         heads = self._heads_of(q)
         mask = self._vector(row_mask, torch.int64, (self.rows,), "row_mask")
         scale = self.cache.head_dim ** -0.5 if scale is None else scale
-        nbytes = via.via_paged_attend_bytes(self._c, heads, window)
-        return self._attend(via.via_paged_attend, q, heads, out, return_lse, (slot, scale), (window, mask), nbytes)
+        return self._attend(via.via_paged_attend, q, heads, out, return_lse, (slot, scale), (window, mask),
+                            (via.via_paged_attend_bytes, heads, window))
 
     def block_means(self, slot, means, block=64):
         """Mean keys of the blocks the rows complete, into ``means`` (fp32 [n_seqs, n_kv_heads,
@@ -185,8 +198,7 @@ class PagedBatch:
         if out is None:
             out = torch.empty((self.rows, kvh, n_sel), dtype=torch.int32, device=q.device)
         dst = self._vector(out, torch.int32, (self.rows, kvh, n_sel), "out")
-        nbytes = via.via_paged_select_bytes(self._c, block)
-        ws = self._workspace(nbytes)
+        ws, nbytes = self._workspace(via.via_paged_select_bytes, block)
         self._call(via.via_paged_select, src, ld, heads, addr, n, block, n_first, n_last, n_sel, dst,
                    ws.data_ptr() if nbytes else None, nbytes)
         return out
@@ -197,6 +209,5 @@ class PagedBatch:
         n_sel = sel.shape[2] if sel.dim() == 3 else 0
         lists = self._vector(sel, torch.int32, (self.rows, self.cache.n_kv_heads, n_sel), "sel")
         scale = self.cache.head_dim ** -0.5 if scale is None else scale
-        nbytes = via.via_paged_attend_blocks_bytes(self._c, heads, block, n_sel)
         return self._attend(via.via_paged_attend_blocks, q, heads, out, return_lse, (slot, scale), (block, lists, n_sel),
-                            nbytes)
+                            (via.via_paged_attend_blocks_bytes, heads, block, n_sel))
