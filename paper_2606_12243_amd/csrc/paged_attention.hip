@@ -540,6 +540,12 @@ __device__ __forceinline__ void lds_copy16(const void* base, uint32_t voff, uint
   asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base), "s"(lds) : "memory", "m0");
 }
 
+// maximum over the lane and its partner, lane ^ 32
+__device__ __forceinline__ float other_half_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __builtin_elementwise_maximum(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
 template <int HD>
 __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   using S = Shape<uint16_t, HD>;
@@ -561,7 +567,16 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   const Query q = query_of(a, g, tile * kTileQueries + wave * 32 + ql, first, n, len);
   const int k0 = lo + split * a.span, k1 = min(end, k0 + a.span);
   if (a.n_splits > 1 && k0 >= end) return;  // the joining kernel does not read it
-  const int top = a.row_mask ? min(len, a.c.cap) : q.vis;  // the query sees no key from here on
+  // no query of the wave sees a key before `from` or from `top` on
+  int from = q.valid ? q.lo : 0x7FFFFFFF, top = !q.valid ? 0 : a.row_mask ? min(len, a.c.cap) : q.vis;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    from = min(from, __shfl_xor(from, o, 64));
+    top = max(top, __shfl_xor(top, o, 64));
+  }
+  from = __builtin_amdgcn_readfirstlane(from);
+  top = __builtin_amdgcn_readfirstlane(top);
+  auto whole = [&](int kb) { return __all(!q.valid || (kb >= q.lo && kb + kTileKeys <= q.vis)); };
 
   uint4 qf[NQ];
   {
@@ -609,21 +624,28 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
     const int pages2 = pages_of(t + 2);
     if (t + 1 < tiles) copy(t + 1, pages1);
     const int kb = k0 + t * kTileKeys;
-    const unsigned char* sk = &smem[t & 1][0][0][0];
-    const unsigned char* sv = &smem[t & 1][1][0][0];
-    if (__any(q.valid && kb < top && kb + kTileKeys > q.lo)) {
+    const unsigned char* sk = &smem[t & 1][0][0][0] + k_at;
+    const unsigned char* sv = &smem[t & 1][1][0][0] + lane * 16;
+    if (kb < top && kb + kTileKeys > from) {
+      const uint32_t absent = (uint32_t)__ballot(pages < 0) & 15;
+      const bool all = !absent && whole(kb);
       f32x16 s[2];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
 #pragma unroll
-        for (int j = 0; j < NQ; ++j) s[b] = mma_bf16(*(const uint4*)(sk + k_at + b * 2 * kPage + j * 512), qf[j], s[b]);
-        __builtin_amdgcn_sched_barrier(0);
+        for (int j = 0; j < NQ; ++j) s[b] = mma_bf16(*(const uint4*)(sk + b * 2 * kPage + j * 512), qf[j], s[b]);
       }
-      const uint64_t absent = __ballot(pages < 0) & 15;
-      const bool whole = !absent && __all(!q.valid || (kb >= q.lo && kb + kTileKeys <= q.vis));
-      if (!whole) {
+      // four operand reads ahead of the products
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+      for (int i = 0; i < 2 * NQ - 4; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+      if (!all) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
           const uint32_t seen = seen_keys<uint16_t>(q, kb + b * 32, !((absent >> (2 * b)) & 1), !((absent >> (2 * b + 1)) & 1), half);
@@ -631,11 +653,16 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
           for (int i = 0; i < 16; ++i) s[b][i] = (seen >> i) & 1 ? s[b][i] : -INFINITY;
         }
       }
-      float bm = fmaxf(s[0][0], s[1][0]);
+      // (maximum, not fmaxf: one instruction for two values, NaN kept)
+      float bm = s[0][0], bm1 = s[1][0];
 #pragma unroll
-      for (int i = 1; i < 16; ++i) bm = fmaxf(bm, fmaxf(s[0][i], s[1][i]));
-      bm = fmaxf(bm, __shfl_xor(bm, 32, 64));
-      const float mn = fmaxf(acc.m, bm * sl2);
+      for (int i = 1; i < 15; i += 2) {
+        bm = __builtin_elementwise_maximum(__builtin_elementwise_maximum(bm, s[0][i]), s[0][i + 1]);
+        bm1 = __builtin_elementwise_maximum(__builtin_elementwise_maximum(bm1, s[1][i]), s[1][i + 1]);
+      }
+      bm = __builtin_elementwise_maximum(__builtin_elementwise_maximum(bm, s[0][15]), bm1);
+      bm = other_half_max(__builtin_elementwise_maximum(bm, s[1][15]));
+      const float mn = __builtin_elementwise_maximum(acc.m, bm * sl2);
       if (__any(mn > acc.m + 8.f)) {  // (from -infinity: at the first key seen)
         const float alpha = mn == acc.m ? 1.f : __builtin_amdgcn_exp2f(acc.m - mn);
 #pragma unroll
@@ -644,43 +671,54 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
         acc.m = mn;
       }
       const float neg_m = acc.m == -INFINITY ? 0.f : -acc.m;
-      uint4 p[4];
+      // half a tile's weights and values at a time: the second half's weights run beside the first half's products
+      uint4 v[2][2 * DT], p[2][2];
+      uint32_t bits = 0;
+      auto values = [&](int b) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t w[4];
+        for (int i = 0; i < 2 * DT; ++i) v[b][i] = *(const uint4*)(sv + (b * 2 + i / DT) * kPage + i % DT * 1024);
+      };
+      auto weights = [&](int b) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = (c & 1) * 8 + 2 * e;
-          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[c >> 1][i], sl2, neg_m));
-          const float p1 = __builtin_amdgcn_exp2f(fmaf(s[c >> 1][i + 1], sl2, neg_m));
-          acc.l += p0;
-          acc.l += p1;
-          const bf16x2 pk = {(__bf16)p0, (__bf16)p1};
-          w[e] = __builtin_bit_cast(uint32_t, pk);
-        }
-        p[c] = make_uint4(w[0], w[1], w[2], w[3]);
-      }
-      if (whole) {
+        for (int c = 0; c < 2; ++c) {
+          uint32_t w[4];
+          float sum[4];
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
-            acc.o[dt] = mma_bf16(*(const uint4*)(sv + c * kPage + dt * 1024 + lane * 16), p[c], acc.o[dt]);
-      } else {
-        uint32_t bits = 0;
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) {
-            const uint4 v = *(const uint4*)(sv + c * kPage + dt * 1024 + lane * 16);
-            bits |= odd_bits<uint16_t>(v.x) | odd_bits<uint16_t>(v.y) | odd_bits<uint16_t>(v.z) | odd_bits<uint16_t>(v.w);
-            const uint4 u = make_uint4(drop_odd<uint16_t>(v.x), drop_odd<uint16_t>(v.y), drop_odd<uint16_t>(v.z),
-                                       drop_odd<uint16_t>(v.w));
-            acc.o[dt] = mma_bf16(u, p[c], acc.o[dt]);
-            __builtin_amdgcn_sched_barrier(0);  // (keeps few of them in registers)
+          for (int e = 0; e < 4; ++e) {
+            const int i = c * 8 + 2 * e;
+            const float p0 = __builtin_amdgcn_exp2f(fmaf(s[b][i], sl2, neg_m));
+            const float p1 = __builtin_amdgcn_exp2f(fmaf(s[b][i + 1], sl2, neg_m));
+            sum[e] = p0 + p1;
+            const bf16x2 pk = {(__bf16)p0, (__bf16)p1};
+            w[e] = __builtin_bit_cast(uint32_t, pk);
           }
-        any_odd |= __any(bits != 0);
-      }
+          acc.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          p[b][c] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      };
+      auto products = [&](int b) {
+#pragma unroll
+        for (int i = 0; i < 2 * DT; ++i) acc.o[i % DT] = mma_bf16(v[b][i], p[b][i / DT], acc.o[i % DT]);
+      };
+      auto clean = [&](int b) {
+        if (!all) {
+#pragma unroll
+          for (int i = 0; i < 2 * DT; ++i) {
+            uint4& x = v[b][i];
+            bits |= odd_bits<uint16_t>(x.x) | odd_bits<uint16_t>(x.y) | odd_bits<uint16_t>(x.z) | odd_bits<uint16_t>(x.w);
+            x = make_uint4(drop_odd<uint16_t>(x.x), drop_odd<uint16_t>(x.y), drop_odd<uint16_t>(x.z), drop_odd<uint16_t>(x.w));
+          }
+        }
+      };
+      values(0);
+      weights(0);
+      clean(0);
+      values(1);
+      products(0);
+      weights(1);
+      clean(1);
+      products(1);
+      any_odd |= __any(bits != 0);
     }
     pages = pages1;
     pages1 = pages2;
@@ -691,7 +729,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
       const int at = pages_of(t);
       // every half of a tile that was not whole
       const int kb = k0 + t * kTileKeys;
-      if (!(__ballot(at < 0) & 15) && __all(!q.valid || (kb >= q.lo && kb + kTileKeys <= q.vis))) continue;
+      if (!(__ballot(at < 0) & 15) && whole(kb)) continue;
 #pragma unroll 1
       for (int b = 0; b < 2; ++b) {
         const int page0 = __builtin_amdgcn_readlane(at, 2 * b), page1 = __builtin_amdgcn_readlane(at, 2 * b + 1);
