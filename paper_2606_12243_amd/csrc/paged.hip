@@ -264,15 +264,18 @@ __global__ __launch_bounds__(64) void paged_means_kernel(MeansArgs a) {
 // the last n_last of them are kept, and of the others the highest scores, ties
 // to the lower block, until n_sel are chosen.
 //
-// A work-group takes 16 rows of a sequence and one K/V head: its eight waves score
-// 16 blocks at a time with v_mfma_f64_16x16x4_f64, the next 16 blocks' means in
-// flight, and then choose for one row after another.  A score is kept as 64 bits
-// that order like it; a wave holds the upper halves of a row's scores in
-// registers and finds the n_sel-th largest bit by bit, which ends as soon as
-// n_sel of them are as large; lower halves are read only where upper ones tie.
-constexpr int kSelectThreads = 512, kSelectWaves = kSelectThreads / 64;
+// Two kernels.  The first scores: a work-group takes 16 rows of a sequence, one
+// K/V head and kScoreBlocks blocks, sums the queries into LDS and lets each wave take
+// 16 blocks at a time with v_mfma_f64_16x16x4_f64.  A score is kept as 64 bits that order
+// like it.  The second chooses, a wave a (row, K/V head): it holds the upper halves of
+// the row's scores in registers and finds the n_sel-th largest bit by bit, which
+// ends as soon as n_sel of them are as large; lower halves are read only where upper
+// ones tie.  (One kernel for both left half the card idle on few rows, and the
+// scores' registers kept the choice from running beside them on many.)
+constexpr int kScoreBlocks = 128;
 constexpr int kSelectHeld = 32;  // scores a lane holds: rows of up to 64 * kSelectHeld blocks
 typedef double f64x4 __attribute__((ext_vector_type(4)));
+typedef double f64x2 __attribute__((ext_vector_type(2)));
 
 // order of the doubles as unsigned numbers; NaN lowest, its upper half above 0
 __device__ __forceinline__ uint64_t sortable(double x) {
@@ -308,153 +311,181 @@ __device__ __forceinline__ void add_to(double (&x)[N], const T* p) {
 }
 
 template <typename T, int HD>
-__global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(SelectArgs a) {
+__global__ __launch_bounds__(256) void paged_score_kernel(SelectArgs a) {
   constexpr int KS = HD / 4;  // k steps; lane l holds dims (l/16) * KS .. + KS - 1 of row or block l % 16
+  constexpr int kRow = HD + 2;  // doubles of a row in LDS (rows 4 banks apart)
+  __shared__ __align__(16) double sq[16 * kRow];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int g = blockIdx.y, m = lane & 15, kq = lane >> 4;
-  const int G = a.H / a.c.KVH;
+  const int g = blockIdx.y, m = lane & 15, kq = lane >> 4, G = a.H / a.c.KVH;
   int seq, tile, first, n, len;
   if (!tile_of_item(a.c, blockIdx.x, 1, 16, seq, tile)) return;
   seq_of_wave(a.c, seq, first, n, len);
   const int r0 = tile * 16;
   if (tile < 0 || r0 >= n) return;
-  const int pos0 = len - n + r0;  // position of the tile's first row
   const int rows = min(16, n - r0);
   // blocks the tile's last row sees (positions past the cap see what the last one does)
-  const int seen = min(min(max(pos0 + rows - 1, -1), a.c.cap - 1) / a.block + 1, a.nb);
-  if (wave * 16 < seen) {
-    const float* means = a.means + ((size_t)seq * a.c.KVH + g) * (size_t)a.max_blocks * HD + kq * KS;
-    float4 v[KS / 4], u[KS / 4];
-    auto load = [&](float4 (&d)[KS / 4], int b0) {
-      const float* p = means + (size_t)min(b0 + m, seen - 1) * HD;
+  const int last = min(max(len - n + r0 + rows - 1, -1), a.c.cap - 1);
+  const int seen = last < 0 ? 0 : min(last / a.block + 1, a.nb);
+  const int from = blockIdx.z * kScoreBlocks, to = min(seen, from + kScoreBlocks);
+  if (from >= to) return;
+  const float* means = a.means + ((size_t)seq * a.c.KVH + g) * (size_t)a.max_blocks * HD + kq * KS;
+  float4 v[KS / 4];
+  auto load = [&](int b0) {
+    const float* p = means + (size_t)min(b0 + m, to - 1) * HD;
 #pragma unroll
-      for (int i = 0; i < KS / 4; ++i) d[i] = *(const float4*)(p + i * 4);
-    };
-    load(v, wave * 16);
-    double q[KS];
+    for (int i = 0; i < KS / 4; ++i) v[i] = *(const float4*)(p + i * 4);
+  };
+  load(min(from + wave * 16, to - 1));
+  {  // the group's summed queries: thread t has dims 8 (t % (HD / 8)) .. + 7 of rows t / (HD / 8), ...
+    constexpr int TPR = HD / 8;
+    for (int r = threadIdx.x / TPR; r < 16; r += 256 / TPR) {
+      const int d = threadIdx.x % TPR * 8;
+      double q[8];
 #pragma unroll
-    for (int i = 0; i < KS; ++i) q[i] = 0.0;
-    if (m < rows) {
-      const T* p = (const T*)a.q + (size_t)(first + r0 + m) * a.q_ld + (size_t)g * G * HD + kq * KS;
-      int h = 0;
-      for (; h + 4 <= G; h += 4) {  // (four heads' loads together)
+      for (int i = 0; i < 8; ++i) q[i] = 0.0;
+      if (r < rows) {
+        const T* p = (const T*)a.q + (size_t)(first + r0 + r) * a.q_ld + (size_t)g * G * HD + d;
+        int h = 0;
+        for (; h + 4 <= G; h += 4) {  // (four heads' loads together)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) add_to<T, KS>(q, p + (size_t)(h + i) * HD);
+          for (int i = 0; i < 4; ++i) add_to<T, 8>(q, p + (size_t)(h + i) * HD);
+        }
+        for (; h < G; ++h) add_to<T, 8>(q, p + (size_t)h * HD);
       }
-      for (; h < G; ++h) add_to<T, KS>(q, p + (size_t)h * HD);
-    }
-    auto score = [&](const float4 (&d)[KS / 4], int b0) {
-      f64x4 s = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll
-      for (int i = 0; i < KS / 4; ++i) {
-        s = __builtin_amdgcn_mfma_f64_16x16x4f64(q[4 * i], (double)d[i].x, s, 0, 0, 0);
-        s = __builtin_amdgcn_mfma_f64_16x16x4f64(q[4 * i + 1], (double)d[i].y, s, 0, 0, 0);
-        s = __builtin_amdgcn_mfma_f64_16x16x4f64(q[4 * i + 2], (double)d[i].z, s, 0, 0, 0);
-        s = __builtin_amdgcn_mfma_f64_16x16x4f64(q[4 * i + 3], (double)d[i].w, s, 0, 0, 0);
-      }
-      // register i of lane l: row 4 i + l / 16, block l % 16
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int row = 4 * i + kq;
-        if (row < rows && b0 + m < seen)
-          a.scores[((size_t)(first + r0 + row) * a.c.KVH + g) * a.nb + b0 + m] = sortable(s[i]);
-      }
-    };
-    constexpr int kStep = kSelectWaves * 16;
-    for (int b0 = wave * 16; b0 < seen; b0 += 2 * kStep) {
-      load(u, b0 + kStep);
-      score(v, b0);
-      if (b0 + kStep >= seen) break;
-      load(v, b0 + 2 * kStep);
-      score(u, b0 + kStep);
+      for (int i = 0; i < 8; i += 2) *(f64x2*)&sq[r * kRow + d + i] = f64x2{q[i], q[i + 1]};
     }
   }
   __syncthreads();
-  for (int r = wave; r < rows; r += kSelectWaves) {
-    const int row = first + r0 + r, pos = min(pos0 + r, a.c.cap - 1);
-    const int vis = pos < 0 ? 0 : min(pos / a.block + 1, a.nb);
-    const uint64_t* sc = a.scores + ((size_t)row * a.c.KVH + g) * a.nb;
-    int32_t* out = a.sel + ((size_t)row * a.c.KVH + g) * a.n_sel;
-    const int rounds = (vis + 63) >> 6;  // block of round j: 64 j + lane
-    auto kept = [&](int b) { return b < a.n_first || b >= vis - a.n_last; };
-    auto read = [&](int b) { return sc[min(b, vis - 1)]; };
-    auto upper = [&](int b, uint64_t k) { return b >= vis ? 0u : kept(b) ? ~0u : (uint32_t)(k >> 32); };
-    auto lower = [&](int b) { return kept(b) ? ~0u : (uint32_t)read(b); };
-    uint32_t held[kSelectHeld];
+  double q[KS];
 #pragma unroll
-    for (int j0 = 0; j0 < kSelectHeld; j0 += 8) {
-      uint64_t k[8];
+  for (int i = 0; i < KS; i += 2) {
+    const f64x2 x = *(const f64x2*)&sq[m * kRow + kq * KS + i];
+    q[i] = x[0];
+    q[i + 1] = x[1];
+  }
+  for (int b0 = from + wave * 16; b0 < to; b0 += 64) {
+    f64x4 s = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+    for (int i = 0; i < KS / 4; ++i) {
+      s = __builtin_amdgcn_mfma_f64_16x16x4f64(q[4 * i], (double)v[i].x, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f64_16x16x4f64(q[4 * i + 1], (double)v[i].y, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f64_16x16x4f64(q[4 * i + 2], (double)v[i].z, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f64_16x16x4f64(q[4 * i + 3], (double)v[i].w, s, 0, 0, 0);
+    }
+    if (b0 + 64 < to) load(b0 + 64);
+    // register i of lane l: row 4 i + l / 16, block l % 16
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = 4 * i + kq;
+      if (row < rows && b0 + m < to)
+        a.scores[((size_t)(first + r0 + row) * a.c.KVH + g) * a.nb + b0 + m] = sortable(s[i]);
+    }
+  }
+}
+
+// sum over the wave, the same in all lanes
+__device__ __forceinline__ int wave_total(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);  // row_shr 1, 2, 4, 8: a row's sum in its last lane
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+  return __builtin_amdgcn_readlane(x, 15) + __builtin_amdgcn_readlane(x, 31) + __builtin_amdgcn_readlane(x, 47) +
+         __builtin_amdgcn_readlane(x, 63);
+}
+
+__global__ __launch_bounds__(256) void paged_choose_kernel(SelectArgs a) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int item = blockIdx.x * 4 + wave, row = item / a.c.KVH, g = item % a.c.KVH;
+  if (row >= a.c.rows) return;
+  const int seq = seq_of_row(a.c, row);
+  if (seq < 0) return;
+  int first, n, len;
+  seq_of_wave(a.c, seq, first, n, len);
+  const int pos = min(len - n + row - first, a.c.cap - 1);
+  const int vis = pos < 0 ? 0 : min(pos / a.block + 1, a.nb);
+  const uint64_t* sc = a.scores + ((size_t)row * a.c.KVH + g) * a.nb;
+  int32_t* out = a.sel + ((size_t)row * a.c.KVH + g) * a.n_sel;
+  const int rounds = (vis + 63) >> 6;  // block of round j: 64 j + lane
+  auto kept = [&](int b) { return b < a.n_first || b >= vis - a.n_last; };
+  auto read = [&](int b) { return sc[min(b, vis - 1)]; };
+  auto upper = [&](int b, uint64_t k) { return b >= vis ? 0u : kept(b) ? ~0u : (uint32_t)(k >> 32); };
+  auto lower = [&](int b) { return kept(b) ? ~0u : (uint32_t)read(b); };
+  uint32_t held[kSelectHeld];
+#pragma unroll
+  for (int j0 = 0; j0 < kSelectHeld; j0 += 8) {
+    uint64_t k[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      held[j0 + j] = 0;
+      if (j0 < rounds) k[j] = read((j0 + j) * 64 + lane);  // (eight reads in flight)
+    }
+    if (j0 < rounds) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        held[j0 + j] = 0;
-        if (j0 < rounds) k[j] = read((j0 + j) * 64 + lane);  // (eight reads in flight)
-      }
-      if (j0 < rounds) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          held[j0 + j] = upper((j0 + j) * 64 + lane, k[j]);
-          __builtin_amdgcn_sched_barrier(0);  // (keeps the comparisons' masks few)
-        }
+        held[j0 + j] = upper((j0 + j) * 64 + lane, k[j]);
+        __builtin_amdgcn_sched_barrier(0);  // (keeps the comparisons' masks few)
       }
     }
-    // f(round, upper half) for every round
-    auto each = [&](auto f) {
-#pragma unroll
-      for (int j0 = 0; j0 < kSelectHeld; j0 += 4) {  // (past the last round they are 0)
-        if (j0 >= rounds) break;
-#pragma unroll
-        for (int j = j0; j < j0 + 4; ++j) f(j, held[j]);
-      }
-      for (int j = kSelectHeld; j < rounds; ++j) f(j, upper(j * 64 + lane, read(j * 64 + lane)));
-    };
-    // chosen: upper halves above hi; of those equal to it, lower halves above lo, and the first `ties` equal to that
-    uint32_t hi = 0, lo = ~0u;
-    int ties = 0;
-    if (vis > a.n_sel) {
-      bool exact = false;
-      for (int bit = 31; bit >= 0 && !exact; --bit) {
-        const uint32_t t = hi | (1u << bit);
-        int c = 0;
-        each([&](int, uint32_t k) { c += __popcll(__ballot(k >= t)); });
-        if (c >= a.n_sel) hi = t;
-        exact = c == a.n_sel;
-      }
-      if (exact) {
-        hi -= 1;
-      } else {
-        int above = 0;
-        each([&](int, uint32_t k) { above += __popcll(__ballot(k > hi)); });
-        const int want = a.n_sel - above;
-        auto tied = [&](uint32_t t) {  // equal upper halves with lower ones >= t
-          int l = lane, c = 0;
-          asm volatile("" : "+v"(l));  // (recomputes the blocks: their masks would not fit the scalar registers)
-          each([&](int j, uint32_t k) { c += __popcll(__ballot(k == hi && lower(j * 64 + l) >= t)); });
-          return c;
-        };
-        lo = 0;
-        for (int bit = 31; bit >= 0; --bit)
-          if (tied(lo | (1u << bit)) >= want) lo |= 1u << bit;
-        ties = want - (lo == ~0u ? 0 : tied(lo + 1));
-      }
-    }
-    int done = 0;
-    const uint64_t before = (1ull << lane) - 1;
-    each([&](int j, uint32_t k) {
-      const int b = j * 64 + lane;
-      bool take = k > hi;  // (0 where the row sees no block)
-      if (ties > 0 || lo != ~0u) {  // (uniform)
-        const bool eq = k == hi;
-        const uint32_t l = eq ? lower(b) : 0u;
-        const uint64_t tied = __ballot(eq && l == lo);
-        take |= eq && (l > lo || (l == lo && __popcll(tied & before) < ties));
-        ties -= min(ties, __popcll(tied));
-      }
-      const uint64_t taken = __ballot(take);
-      if (take) out[done + __popcll(taken & before)] = b;
-      done += __popcll(taken);
-    });
-    for (int i = done + lane; i < a.n_sel; i += 64) out[i] = -1;
   }
+  // f(round, upper half) for every round
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int j0 = 0; j0 < kSelectHeld; j0 += 4) {  // (past the last round they are 0)
+      if (j0 >= rounds) break;
+#pragma unroll
+      for (int j = j0; j < j0 + 4; ++j) f(j, held[j]);
+    }
+    for (int j = kSelectHeld; j < rounds; ++j) f(j, upper(j * 64 + lane, read(j * 64 + lane)));
+  };
+  // chosen: upper halves above hi; of those equal to it, lower halves above lo, and the first `ties` equal to that
+  uint32_t hi = 0, lo = ~0u;
+  int ties = 0;
+  if (vis > a.n_sel) {
+    bool exact = false;
+    for (int bit = 31; bit >= 0 && !exact; --bit) {
+      const uint32_t t = hi | (1u << bit);
+      int c = 0;
+      each([&](int, uint32_t k) { c += k >= t; });
+      c = wave_total(c);
+      if (c >= a.n_sel) hi = t;
+      exact = c == a.n_sel;
+    }
+    if (exact) {
+      hi -= 1;
+    } else {
+      int above = 0;
+      each([&](int, uint32_t k) { above += k > hi; });
+      const int want = a.n_sel - wave_total(above);
+      auto tied = [&](uint32_t t) {  // equal upper halves with lower ones >= t
+        int l = lane, c = 0;
+        asm volatile("" : "+v"(l));  // (recomputes the blocks: their masks would not fit the scalar registers)
+        each([&](int j, uint32_t k) { c += k == hi && lower(j * 64 + l) >= t; });
+        return wave_total(c);
+      };
+      lo = 0;
+      for (int bit = 31; bit >= 0; --bit)
+        if (tied(lo | (1u << bit)) >= want) lo |= 1u << bit;
+      ties = want - (lo == ~0u ? 0 : tied(lo + 1));
+    }
+  }
+  int done = 0;
+  const uint64_t before = (1ull << lane) - 1;
+  each([&](int j, uint32_t k) {
+    const int b = j * 64 + lane;
+    bool take = k > hi;  // (0 where the row sees no block)
+    if (ties > 0 || lo != ~0u) {  // (uniform)
+      const bool eq = k == hi;
+      const uint32_t l = eq ? lower(b) : 0u;
+      const uint64_t tied = __ballot(eq && l == lo);
+      take |= eq && (l > lo || (l == lo && __popcll(tied & before) < ties));
+      ties -= min(ties, __popcll(tied));
+    }
+    const uint64_t taken = __ballot(take);
+    if (take) out[done + __popcll(taken & before)] = b;
+    done += __popcll(taken);
+  });
+  for (int i = done + lane; i < a.n_sel; i += 64) out[i] = -1;
 }
 
 constexpr int kAppendGroups = 2048;
@@ -488,12 +519,16 @@ void launch_paged_means(bool bf16, const MeansArgs& a, hipStream_t s) {
 }
 
 void launch_paged_select(bool bf16, const SelectArgs& a, hipStream_t s) {
-  const dim3 grid((a.c.rows + 15) / 16 + a.c.n_seqs, a.c.KVH);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kSelectThreads), 0, s, a); };
-  if (bf16)
-    a.hd == 128 ? go(paged_select_kernel<uint16_t, 128>) : go(paged_select_kernel<uint16_t, 64>);
-  else
-    a.hd == 128 ? go(paged_select_kernel<float, 128>) : go(paged_select_kernel<float, 64>);
+  const dim3 grid((a.c.rows + 15) / 16 + a.c.n_seqs, a.c.KVH, (a.nb + kScoreBlocks - 1) / kScoreBlocks);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a); };
+  if (a.nb > 0) {
+    if (bf16)
+      a.hd == 128 ? go(paged_score_kernel<uint16_t, 128>) : go(paged_score_kernel<uint16_t, 64>);
+    else
+      a.hd == 128 ? go(paged_score_kernel<float, 128>) : go(paged_score_kernel<float, 64>);
+  }
+  const int items = a.c.rows * a.c.KVH;
+  hipLaunchKernelGGL(paged_choose_kernel, dim3((items + 3) / 4), dim3(256), 0, s, a);
 }
 
 }  // namespace via
