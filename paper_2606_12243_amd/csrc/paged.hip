@@ -265,14 +265,16 @@ __global__ __launch_bounds__(64) void paged_means_kernel(MeansArgs a) {
 // to the lower block, until n_sel are chosen.
 //
 // Two kernels.  The first scores: a work-group takes 16 rows of a sequence, one
-// K/V head and kScoreBlocks blocks, sums the queries into LDS and lets each wave take
+// K/V head and some of the blocks, sums the queries into LDS and lets each wave take
 // 16 blocks at a time with v_mfma_f64_16x16x4_f64.  A score is kept as 64 bits that order
 // like it.  The second chooses, a wave a (row, K/V head): it holds the upper halves of
 // the row's scores in registers and finds the n_sel-th largest bit by bit, which
 // ends as soon as n_sel of them are as large; lower halves are read only where upper
 // ones tie.  (One kernel for both left half the card idle on few rows, and the
 // scores' registers kept the choice from running beside them on many.)
-constexpr int kScoreBlocks = 128;
+// Work-groups a launch aims for: fewer, with more blocks each, share the queries'
+// sums and the wait for them among more products.
+constexpr int kScoreGroups = 1024;
 constexpr int kSelectHeld = 32;  // scores a lane holds: rows of up to 64 * kSelectHeld blocks
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 typedef double f64x2 __attribute__((ext_vector_type(2)));
@@ -311,7 +313,7 @@ __device__ __forceinline__ void add_to(double (&x)[N], const T* p) {
 }
 
 template <typename T, int HD>
-__global__ __launch_bounds__(256) void paged_score_kernel(SelectArgs a) {
+__global__ __launch_bounds__(256) void paged_score_kernel(SelectArgs a, int per) {
   constexpr int KS = HD / 4;  // k steps; lane l holds dims (l/16) * KS .. + KS - 1 of row or block l % 16
   constexpr int kRow = HD + 2;  // doubles of a row in LDS (rows 4 banks apart)
   __shared__ __align__(16) double sq[16 * kRow];
@@ -326,7 +328,7 @@ __global__ __launch_bounds__(256) void paged_score_kernel(SelectArgs a) {
   // blocks the tile's last row sees (positions past the cap see what the last one does)
   const int last = min(max(len - n + r0 + rows - 1, -1), a.c.cap - 1);
   const int seen = last < 0 ? 0 : min(last / a.block + 1, a.nb);
-  const int from = blockIdx.z * kScoreBlocks, to = min(seen, from + kScoreBlocks);
+  const int from = blockIdx.z * per, to = min(seen, from + per);
   if (from >= to) return;
   const float* means = a.means + ((size_t)seq * a.c.KVH + g) * (size_t)a.max_blocks * HD + kq * KS;
   float4 v[KS / 4];
@@ -519,8 +521,12 @@ void launch_paged_means(bool bf16, const MeansArgs& a, hipStream_t s) {
 }
 
 void launch_paged_select(bool bf16, const SelectArgs& a, hipStream_t s) {
-  const dim3 grid((a.c.rows + 15) / 16 + a.c.n_seqs, a.c.KVH, (a.nb + kScoreBlocks - 1) / kScoreBlocks);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a); };
+  // blocks of a work-group: a multiple of the 64 that its waves score at a time
+  const int tiles = (a.c.rows + 15) / 16 + a.c.n_seqs;
+  const int parts = std::max(1, kScoreGroups / std::max(1, (int)std::min<long long>((long long)tiles * a.c.KVH, kScoreGroups)));
+  const int per = ((a.nb + parts - 1) / parts + 63) / 64 * 64;
+  const dim3 grid(tiles, a.c.KVH, per ? (a.nb + per - 1) / per : 1);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a, per); };
   if (a.nb > 0) {
     if (bf16)
       a.hd == 128 ? go(paged_score_kernel<uint16_t, 128>) : go(paged_score_kernel<uint16_t, 64>);
