@@ -146,6 +146,17 @@ __device__ __forceinline__ void seq_of_wave(const PagedRef& c, int s, int& first
   len = __builtin_amdgcn_readfirstlane(seq_len(c, s));
 }
 
+// Lets the matrix instructions before it finish (16 passes at most, 19 wait states).
+// Their results may not be read earlier, and the compiler counts the wait states
+// too low where the read is in another basic block that several paths lead to
+// (fp32 scores after the branch around the masks: the last one was read 7
+// states after the instruction and was wrong).
+__device__ __forceinline__ void settle() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 15\n\ts_nop 3");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // Page of a sequence's positions 16 i .. 16 i + 15; -1 where the table names
 // none, which every kernel leaves alone.
 __device__ __forceinline__ int page_of(const PagedRef& c, int seq, int i) {

@@ -381,6 +381,7 @@ __global__ __launch_bounds__(256) void paged_score_kernel(SelectArgs a, int per)
       s = __builtin_amdgcn_mfma_f64_16x16x4f64(q[4 * i + 2], (double)v[i].z, s, 0, 0, 0);
       s = __builtin_amdgcn_mfma_f64_16x16x4f64(q[4 * i + 3], (double)v[i].w, s, 0, 0, 0);
     }
+    settle();
     if (b0 + 64 < to) load(b0 + 64);
     // register i of lane l: row 4 i + l / 16, block l % 16
 #pragma unroll

@@ -224,6 +224,7 @@ __device__ __forceinline__ void add_odd_values(const PagedRef& c, int g, int pag
 #pragma unroll
       for (int i = 0; i < 16; ++i) count[i] = 0.f;
       count = add_pv<T, HD>(f, [&](int i) { return (0u - ((seen >> i) & 1)) & kOne; }, count);
+      settle();
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         a.o[dt][i] += count[i] > 0.f ? add : 0.f;
@@ -256,6 +257,7 @@ __device__ __forceinline__ void compute_block(Block<T, HD>& b, int kb, bool page
       for (int e = 0; e < 4; ++e) s = mma_f32(lane_f(b.k[j], e), lane_f(qj, e), s);
     }
   }
+  settle();
   if (!sees_whole(q, kb, page0, page1)) {
     const uint32_t seen = seen_keys<T>(q, kb, page0, page1, half);
 #pragma unroll
@@ -459,6 +461,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void paged_stream_ke
     }
   }
 
+  settle();
   // merge the four waves in a fixed order: (w0 + w2) + (w1 + w3)
   float lt = acc.l + __shfl_xor(acc.l, 32, 64);
   float mx = acc.m;
@@ -645,6 +648,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
         __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
       __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+      settle();
       if (!all) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
@@ -723,6 +727,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
     pages = pages1;
     pages1 = pages2;
   }
+  settle();
   if (any_odd) {  // (the same in all lanes)
 #pragma unroll 1
     for (int t = 0; t < tiles; ++t) {
