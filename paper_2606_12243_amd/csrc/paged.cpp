@@ -94,13 +94,19 @@ via_status launched(const char* what) {
 // least kMinSpan.
 constexpr int kTargetGroups = 512;
 constexpr int kMinSpan = 128;
+constexpr int kMinTileSpan = 256;
+constexpr int kMaxSpan = 8192;  // ... and, of several sequences, at most
 struct Split {
   long long n_items;  // tiles a launch covers per K/V head
-  int span, n_splits, tile_q;
+  int span, n_splits, tile_q, terms;
 };
-// Rows times heads of a K/V head from which (on average over the sequences) a bf16 call
-// takes the kernel for many rows.
-constexpr int kManyQueries = 128;
+// Queries of a K/V head and sequence (rows times heads, on average over the sequences)
+// from which a bf16 call takes the 128-query kernel: one more than the streaming
+// kernel's 32 share of the keys (16 sequences of 8192 keys, 36 queries: 111 against 143 us;
+// one of 4096: 18 both) ...
+constexpr int kTileFrom = kPagedQueries + 1;
+// ... and from which that holds its weights to one bf16 value.
+constexpr int kOneTermFrom = 128;
 Split split_of(const via_paged* c, int n_heads, int window, int n_sel, int block) {
   Split s{};
   const int G = n_heads / c->n_kv_heads;
@@ -112,7 +118,8 @@ Split split_of(const via_paged* c, int n_heads, int window, int n_sel, int block
     s.tile_q = kPagedQueries;
   } else {
     const long long each = ((long long)c->rows + c->n_seqs - 1) / std::max(1, c->n_seqs);
-    s.tile_q = c->dtype == VIA_DTYPE_BF16 && each * G >= kManyQueries ? kPagedTileQueries : kPagedQueries;
+    s.tile_q = c->dtype == VIA_DTYPE_BF16 && each * G >= kTileFrom ? kPagedTileQueries : kPagedQueries;
+    s.terms = each * G >= kOneTermFrom ? 1 : 2;
     s.n_items = (long long)c->rows * G / s.tile_q + c->n_seqs;
     tiles = (each * G + s.tile_q - 1) / s.tile_q * c->n_seqs;
     keys = cap_of(c);
@@ -121,7 +128,10 @@ Split split_of(const via_paged* c, int n_heads, int window, int n_sel, int block
   }
   const long long groups = std::max<long long>(1, tiles * c->n_kv_heads);
   const long long want = std::min<long long>(std::max<long long>(1, kTargetGroups / groups), kMaxSplits);
-  long long span = std::max<long long>((keys + want - 1) / want, kMinSpan);
+  long long span = (keys + want - 1) / want;
+  // sequences may differ: a short batch's long one must not run on its own at the end
+  if (c->n_seqs > 1 && n_sel == 0) span = std::min(span, std::max<long long>(kMaxSpan, (keys + kMaxSplits - 1) / kMaxSplits));
+  span = std::max<long long>(span, s.tile_q == kPagedQueries ? kMinSpan : kMinTileSpan);
   span = (span + 127) / 128 * 128;  // four waves' blocks
   s.span = (int)span;
   s.n_splits = (int)std::max<long long>(1, (keys + span - 1) / span);
@@ -146,6 +156,7 @@ via_status attention(const via_paged* c, int slot, PagedAttnArgs& a, void* works
   a.n_splits = s.n_splits;
   a.n_items = (int)s.n_items;
   a.tile_q = s.tile_q;
+  a.terms = s.terms;
   a.part_o = (float*)workspace;
   a.part_ml = (float*)workspace + (size_t)s.n_splits * c->rows * a.H * c->head_dim;
   launch_paged_attention(c->dtype == VIA_DTYPE_BF16, a, (hipStream_t)stream);

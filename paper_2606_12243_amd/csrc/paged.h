@@ -60,6 +60,7 @@ struct PagedAttnArgs {
   int span, n_splits;
   int n_items;  // tiles a launch covers per K/V head
   int tile_q;   // queries of a tile: kPagedQueries or kPagedTileQueries
+  int terms;    // bf16 values that a weight is held to in the latter
   float* part_o;   // [n_splits][rows][H][hd]
   float* part_ml;  // [n_splits][rows][H][2]: maximum (log2 units), sum
 };

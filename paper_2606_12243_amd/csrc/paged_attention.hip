@@ -125,6 +125,16 @@ struct Acc {
   float m, l;  // running maximum (log2 units) and sum
 };
 
+// Two weights as bf16: rounded to nearest, or (hi, lo) truncated and the rest rounded.
+__device__ __forceinline__ uint32_t round_pair(float p0, float p1) {
+  const bf16x2 r = {(__bf16)p0, (__bf16)p1};
+  return __builtin_bit_cast(uint32_t, r);
+}
+__device__ __forceinline__ uint32_t split_pair(float p0, float p1, uint32_t& lo) {
+  lo = round_pair(p0 - __uint_as_float(__float_as_uint(p0) & 0xFFFF0000u), p1 - __uint_as_float(__float_as_uint(p1) & 0xFFFF0000u));
+  return __builtin_amdgcn_perm(__float_as_uint(p1), __float_as_uint(p0), 0x07060302u);
+}
+
 // O^T += V^T P^T for weights given as a function of the score register
 template <typename T, int HD, typename P>
 __device__ __forceinline__ f32x16 add_pv(const uint4 (&v)[Shape<T, HD>::NV], P p, f32x16 o) {
@@ -292,13 +302,7 @@ __device__ __forceinline__ void compute_block(Block<T, HD>& b, int kb, bool page
     for (int n = 0; n < 2; ++n) {
       uint32_t hw[4], lw[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float p0 = p[n * 8 + 2 * e], p1 = p[n * 8 + 2 * e + 1];
-        hw[e] = __builtin_amdgcn_perm(__float_as_uint(p1), __float_as_uint(p0), 0x07060302u);  // truncated
-        const bf16x2 lo = {(__bf16)(p0 - __uint_as_float(__float_as_uint(p0) & 0xFFFF0000u)),
-                           (__bf16)(p1 - __uint_as_float(__float_as_uint(p1) & 0xFFFF0000u))};
-        lw[e] = __builtin_bit_cast(uint32_t, lo);
-      }
+      for (int e = 0; e < 4; ++e) hw[e] = split_pair(p[n * 8 + 2 * e], p[n * 8 + 2 * e + 1], lw[e]);
       const uint4 hi = make_uint4(hw[0], hw[1], hw[2], hw[3]), lo = make_uint4(lw[0], lw[1], lw[2], lw[3]);
 #pragma unroll
       for (int dt = 0; dt < S::DT; ++dt) {
@@ -525,17 +529,17 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void paged_stream_ke
 }
 
 // ---------------------------------------------------------------------------
-// Many rows, bf16: the matrix instructions bound it.  A work-group takes 128
+// More than 32 queries, bf16: with many rows the matrix instructions bound it.  A work-group takes 128
 // queries of one K/V head, a wave 32 of them; 64 keys at a time are copied into LDS
 // (asynchronously, the next 64 in flight) and read by all four waves as matrix
 // operands.  Pages are copied as they are, but that the two 16-byte halves of a V
 // row go apart, so that every operand read is 256 consecutive bytes per 16 lanes.
 // Two work-groups share a compute unit: one's softmax runs beside the other's
-// products.  P is rounded to one bf16 term here (to nearest; its error, 2^-9 of a
-// weight at most, is below the output's own rounding when a few keys share
-// the weight): two terms are half again the products.  The running maximum is
-// raised only when it grows by more than 2^8, which spares most rescalings of O;
-// weights up to 2^8 lose nothing.
+// products.  The weights are one bf16 value each (TERMS = 1, to nearest: 2^-9 of
+// a weight at most, about what the output's own rounding costs, where two would be
+// half again the products), or two where few rows leave the loop waiting for
+// memory.  The running maximum is raised only when it grows by more than 2^8,
+// which spares most rescalings of O; weights up to 2^8 lose nothing.
 constexpr int kTileQueries = kPagedTileQueries, kTileKeys = 64;
 
 // 16 bytes a lane from base + voff to LDS at lds + 16 * lane (base, lds wave-uniform)
@@ -549,7 +553,7 @@ __device__ __forceinline__ float other_half_max(float x) {
   return __builtin_elementwise_maximum(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-template <int HD>
+template <int HD, int TERMS>
 __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   using S = Shape<uint16_t, HD>;
   constexpr int DT = S::DT, NQ = S::NQ, kPage = kBlock * HD * 2;  // bytes of a K or V page
@@ -676,7 +680,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
       }
       const float neg_m = acc.m == -INFINITY ? 0.f : -acc.m;
       // half a tile's weights and values at a time: the second half's weights run beside the first half's products
-      uint4 v[2][2 * DT], p[2][2];
+      uint4 v[2][2 * DT], p[2][2], p2[2][2];
       uint32_t bits = 0;
       auto values = [&](int b) {
 #pragma unroll
@@ -685,7 +689,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
       auto weights = [&](int b) {
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          uint32_t w[4];
+          uint32_t w[4], w2[4];
           float sum[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -693,16 +697,19 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
             const float p0 = __builtin_amdgcn_exp2f(fmaf(s[b][i], sl2, neg_m));
             const float p1 = __builtin_amdgcn_exp2f(fmaf(s[b][i + 1], sl2, neg_m));
             sum[e] = p0 + p1;
-            const bf16x2 pk = {(__bf16)p0, (__bf16)p1};
-            w[e] = __builtin_bit_cast(uint32_t, pk);
+            w[e] = TERMS == 2 ? split_pair(p0, p1, w2[e]) : round_pair(p0, p1);
           }
+          if constexpr (TERMS == 2) p2[b][c] = make_uint4(w2[0], w2[1], w2[2], w2[3]);
           acc.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
           p[b][c] = make_uint4(w[0], w[1], w[2], w[3]);
         }
       };
       auto products = [&](int b) {
 #pragma unroll
-        for (int i = 0; i < 2 * DT; ++i) acc.o[i % DT] = mma_bf16(v[b][i], p[b][i / DT], acc.o[i % DT]);
+        for (int i = 0; i < 2 * DT; ++i) {
+          acc.o[i % DT] = mma_bf16(v[b][i], p[b][i / DT], acc.o[i % DT]);
+          if constexpr (TERMS == 2) acc.o[i % DT] = mma_bf16(v[b][i], p2[b][i / DT], acc.o[i % DT]);
+        }
       };
       auto clean = [&](int b) {
         if (!all) {
@@ -837,8 +844,10 @@ template <typename T, int HD, bool LISTED>
 void launch(const PagedAttnArgs& a, hipStream_t s) {
   const int blocks = a.n_items * a.c.KVH * a.n_splits;
   if constexpr (sizeof(T) == 2 && !LISTED) {
-    if (a.tile_q == kTileQueries)
-      hipLaunchKernelGGL(paged_tile_kernel<HD>, dim3(blocks), dim3(256), 0, s, a);
+    if (a.tile_q == kTileQueries && a.terms == 2)
+      hipLaunchKernelGGL((paged_tile_kernel<HD, 2>), dim3(blocks), dim3(256), 0, s, a);
+    else if (a.tile_q == kTileQueries)
+      hipLaunchKernelGGL((paged_tile_kernel<HD, 1>), dim3(blocks), dim3(256), 0, s, a);
     else
       hipLaunchKernelGGL((paged_stream_kernel<T, HD, LISTED>), dim3(blocks), dim3(256), 0, s, a);
   } else {
