@@ -11,8 +11,8 @@
 // spans where there are too few tiles to fill the card, and a second kernel
 // joins the partial results in span order.
 //
-// Four waves a work-group; wave w takes the 32-key blocks w, w + 4, ... with
-// the next block's loads in flight.  S^T = K Q^T keeps one query a lane (two
+// Four waves a work-group; wave w takes the 32-key blocks w, w + 4, ... (bf16:
+// with the next block's loads in flight).  S^T = K Q^T keeps one query a lane (two
 // lanes a query, 16 keys each), so a running maximum and sum needs one lane
 // exchange, and its registers are the P^T operand of O^T += V^T P^T as they are:
 //   bf16, v_mfma_f32_32x32x16_bf16: A-row m of the K tile holds key
@@ -106,6 +106,13 @@ __device__ __forceinline__ void load_block(Block<T, HD>& b, const PagedRef& c, i
     for (int dt = 0; dt < S::DT; ++dt) b.v[dt][n] = load_stream(vp + dt * 32 * kBlock);
   }
 }
+
+// Two register sets for a wave's blocks, or one and other waves to run meanwhile: an
+// fp32 block is twice as large, and two of them are spilled at a head of 128 (16 x
+// 4096 keys of 8 heads: 291 us against 122) and leave one work-group a compute unit at 64
+// (64 us against 59).
+template <typename T>
+constexpr bool kTwoSets = sizeof(T) == 2;
 
 // What the lane's query sees: keys [lo, vis), and key base + o where bit o of mask is set.
 struct Query {
@@ -346,7 +353,7 @@ __device__ __forceinline__ Query query_of(const PagedAttnArgs& a, int g, int qi,
 }
 
 template <typename T, int HD, bool LISTED>
-__global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void paged_stream_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(256, (sizeof(T) * HD <= 256 ? 2 : 1)) void paged_stream_kernel(PagedAttnArgs a) {
   using S = Shape<T, HD>;
   constexpr int DT = S::DT;
   const int G = a.H / a.c.KVH;
@@ -430,9 +437,6 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void paged_stream_ke
       }
     }
     __syncthreads();
-    // Two register sets: the next block's loads are in flight while one is
-    // multiplied.  Past the wave's last block it reads that one again, so that
-    // every load is unconditional.
     const int cnt = nblk > wave ? (nblk - wave + 3) >> 2 : 0;
     if (cnt > 0) {
       auto blk = [&](int i) { return wave + 4 * min(i, cnt - 1); };
@@ -444,14 +448,24 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void paged_stream_ke
         const int kb = LISTED ? sbase[blk(i)] : c0 + blk(i) * 32;
         compute_block<T, HD>(b, kb, spage[2 * blk(i)] >= 0, spage[2 * blk(i) + 1] >= 0, q, sq, lane, sl2, acc, odd);
       };
-      Block<T, HD> b0, b1;
-      load(b0, 0);
-      for (int i = 0; i < cnt; i += 2) {
-        load(b1, i + 1);
-        compute(b0, i);
-        if (i + 1 >= cnt) break;
-        load(b0, i + 2);
-        compute(b1, i + 1);
+      if constexpr (kTwoSets<T>) {
+        // the next block's loads are in flight while one is multiplied; past the
+        // wave's last block it reads that one again, so that every load is unconditional
+        Block<T, HD> b0, b1;
+        load(b0, 0);
+        for (int i = 0; i < cnt; i += 2) {
+          load(b1, i + 1);
+          compute(b0, i);
+          if (i + 1 >= cnt) break;
+          load(b0, i + 2);
+          compute(b1, i + 1);
+        }
+      } else {
+        Block<T, HD> b;
+        for (int i = 0; i < cnt; ++i) {
+          load(b, i);
+          compute(b, i);
+        }
       }
       if (odd) {  // (the same in all lanes)
 #pragma unroll 1
