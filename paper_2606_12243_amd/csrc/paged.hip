@@ -319,8 +319,8 @@ __device__ __forceinline__ void add_to(double (&x)[N], const T* p) {
 }
 
 template <typename T, int HD>
-__global__ __launch_bounds__(256) void paged_score_kernel(SelectArgs a, int per) {
-  constexpr int KS = HD / 4;  // k steps; lane l holds dims (l/16) * KS .. + KS - 1 of row or block l % 16
+__global__ __launch_bounds__(256, 4) void paged_score_kernel(SelectArgs a, int per) {
+  constexpr int KS = HD / 4;  // k steps; lane l holds dims 16 i + 4 (l/16) .. + 3 of row or block l % 16
   constexpr int kRow = HD + 2;  // doubles of a row in LDS (rows 4 banks apart)
   __shared__ __align__(16) double sq[16 * kRow];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -336,12 +336,12 @@ __global__ __launch_bounds__(256) void paged_score_kernel(SelectArgs a, int per)
   const int seen = last < 0 ? 0 : min(last / a.block + 1, a.nb);
   const int from = blockIdx.z * per, to = min(seen, from + per);
   if (from >= to) return;
-  const float* means = a.means + ((size_t)seq * a.c.KVH + g) * (size_t)a.max_blocks * HD + kq * KS;
+  const float* means = a.means + ((size_t)seq * a.c.KVH + g) * (size_t)a.max_blocks * HD + kq * 4;
   float4 v[KS / 4];
   auto load = [&](int b0) {
     const float* p = means + (size_t)min(b0 + m, to - 1) * HD;
 #pragma unroll
-    for (int i = 0; i < KS / 4; ++i) v[i] = *(const float4*)(p + i * 4);
+    for (int i = 0; i < KS / 4; ++i) v[i] = *(const float4*)(p + i * 16);
   };
   load(min(from + wave * 16, to - 1));
   {  // the group's summed queries: thread t has dims 8 (t % (HD / 8)) .. + 7 of rows t / (HD / 8), ...
@@ -368,7 +368,7 @@ __global__ __launch_bounds__(256) void paged_score_kernel(SelectArgs a, int per)
   double q[KS];
 #pragma unroll
   for (int i = 0; i < KS; i += 2) {
-    const f64x2 x = *(const f64x2*)&sq[m * kRow + kq * KS + i];
+    const f64x2 x = *(const f64x2*)&sq[m * kRow + (i >> 2) * 16 + kq * 4 + (i & 3)];
     q[i] = x[0];
     q[i + 1] = x[1];
   }
@@ -393,17 +393,7 @@ __global__ __launch_bounds__(256) void paged_score_kernel(SelectArgs a, int per)
   }
 }
 
-// sum over the wave, the same in all lanes
-__device__ __forceinline__ int wave_total(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);  // row_shr 1, 2, 4, 8: a row's sum in its last lane
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
-  return __builtin_amdgcn_readlane(x, 15) + __builtin_amdgcn_readlane(x, 31) + __builtin_amdgcn_readlane(x, 47) +
-         __builtin_amdgcn_readlane(x, 63);
-}
-
-__global__ __launch_bounds__(256) void paged_choose_kernel(SelectArgs a) {
+__global__ __launch_bounds__(256, 8) void paged_choose_kernel(SelectArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int item = blockIdx.x * 4 + wave, row = item / a.c.KVH, g = item % a.c.KVH;
   if (row >= a.c.rows) return;
@@ -455,8 +445,7 @@ __global__ __launch_bounds__(256) void paged_choose_kernel(SelectArgs a) {
     for (int bit = 31; bit >= 0 && !exact; --bit) {
       const uint32_t t = hi | (1u << bit);
       int c = 0;
-      each([&](int, uint32_t k) { c += k >= t; });
-      c = wave_total(c);
+      each([&](int, uint32_t k) { c += __popcll(__ballot(k >= t)); });
       if (c >= a.n_sel) hi = t;
       exact = c == a.n_sel;
     }
@@ -464,13 +453,13 @@ __global__ __launch_bounds__(256) void paged_choose_kernel(SelectArgs a) {
       hi -= 1;
     } else {
       int above = 0;
-      each([&](int, uint32_t k) { above += k > hi; });
-      const int want = a.n_sel - wave_total(above);
+      each([&](int, uint32_t k) { above += __popcll(__ballot(k > hi)); });
+      const int want = a.n_sel - above;
       auto tied = [&](uint32_t t) {  // equal upper halves with lower ones >= t
         int l = lane, c = 0;
         asm volatile("" : "+v"(l));  // (recomputes the blocks: their masks would not fit the scalar registers)
-        each([&](int j, uint32_t k) { c += k == hi && lower(j * 64 + l) >= t; });
-        return wave_total(c);
+        each([&](int j, uint32_t k) { c += __popcll(__ballot(k == hi && lower(j * 64 + l) >= t)); });
+        return c;
       };
       lo = 0;
       for (int bit = 31; bit >= 0; --bit)

@@ -532,3 +532,44 @@ def test_select_with_nan_scores_only():
         got = on_gpu(b).select_blocks(q.cuda(), m.cuda(), n_sel, block=32)
         torch.cuda.synchronize()
         assert torch.equal(got.cpu(), ref.select(b, q, m, n_sel, 32, 1, 2)), n_sel
+
+
+@pytest.mark.parametrize("case", ["all equal", "64 equal", "65 equal", "zero", "small", "tiny", "large", "huge", "wide", "close",
+                                  "one infinite"])
+@pytest.mark.parametrize("dtype,hd", [(BF16, 128), (F32, 64)])
+def test_select_where_32_bits_do_not_decide(dtype, hd, case):
+    """Equal and nearly equal scores, few and many of them around the last place, and sizes at which 32-bit
+    products, squares or sums underflow or overflow: the blocks are those of the 64-bit scores."""
+    say("select undecided", dtype, hd, case)
+    H, KVH, block, n_sel = 4, 2, 32, 40
+    b = ref.Batch(dtype, H, KVH, hd, [3], [16], seed=len(case))
+    b.lens, b.max_kv = [32 * 300 + 3], 32 * 300 + 3
+    b.kv_len = torch.tensor(b.lens, dtype=torch.int32)
+    b.table = torch.zeros((1, 700), dtype=torch.int32)
+    m = b.randn(1, KVH, 301, hd)
+    q = b.randn(b.T, H, hd).to(dtype)
+    best = q.float().view(b.T, KVH, -1, hd).sum(2)[1]  # a mean along the queries of row 1
+    if case == "all equal":
+        m[:] = m[:, :, :1].clone()
+    elif "equal" in case:  # 30 better ones, then as many equal ones as it says
+        n = int(case.split()[0])
+        at = torch.randperm(280, generator=b.g)[:n + 30] + 5
+        m *= 0.01
+        m[0, :, at[:30]] = best[:, None] * (2 + 0.01 * torch.arange(30.0)[:, None])
+        m[0, :, at[30:]] = best[:, None]
+    elif case == "zero":
+        m[:] = 0
+    elif case == "wide":
+        m *= torch.exp(b.randn(1, KVH, 301, 1) * 20)
+    elif case == "close":  # steps of 2^-26 of the score
+        m[:] = best[:, None] * 1024
+        step = torch.randperm(301, generator=b.g).float() * 2.0 ** -17
+        m[0, :, :, 0] += step * best[:, :1].sign()
+    elif case == "one infinite":
+        m[0, 0, 77, 3], m[0, 1, 78, 5] = math.inf, -math.inf
+    else:
+        m *= {"small": 1e-19, "tiny": 1e-38, "large": 1e18, "huge": 1e36}[case]
+        q = (q.float() * {"small": 1e-3, "tiny": 1e-2, "large": 1e3, "huge": 1e3}[case]).to(dtype)
+    got = on_gpu(b).select_blocks(q.cuda(), m.cuda(), n_sel, block=block, n_first=1, n_last=2)
+    torch.cuda.synchronize()
+    assert torch.equal(got.cpu(), ref.select(b, q, m, n_sel, block, 1, 2))

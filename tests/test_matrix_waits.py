@@ -19,7 +19,8 @@ CSRC = os.path.join(ROOT, "paper_2606_12243_amd", "csrc")
 HIPCC = "/opt/rocm/bin/hipcc" if os.path.exists("/opt/rocm/bin/hipcc") else shutil.which("hipcc")
 
 # wait states from a matrix instruction to a read of its result (8 and 16 passes; fp64)
-WAIT = {"v_mfma_f32_32x32x16_bf16": 11, "v_mfma_f32_32x32x2_f32": 18, "v_mfma_f64_16x16x4_f64": 19}
+WAIT = {"v_mfma_f32_32x32x16_bf16": 11, "v_mfma_f32_32x32x2_f32": 18, "v_mfma_f32_16x16x4_f32": 10,
+        "v_mfma_f64_16x16x4_f64": 19}
 STORES = ("ds_write", "global_store", "buffer_store", "scratch_store", "flat_store")
 
 
