@@ -282,7 +282,8 @@ via_status via_dimr_cost(const float *q_logits, const float *p_logits, int32_t r
  * in elements; they and their rows are 16-byte aligned (EINVAL).  n_heads is a
  * multiple of n_kv_heads, query head h reading K/V head h / (n_heads /
  * n_kv_heads).  head_dim is 64 or 128, at most 65535 sequences and
- * 2^27 rows (EUNSUPPORTED). */
+ * 2^27 rows, and rows times heads below 2^24 for the attention and the choice of
+ * blocks (EUNSUPPORTED). */
 typedef struct {
   void *pool;
   int32_t dtype, n_slots, n_blocks, n_kv_heads, head_dim;
@@ -317,13 +318,17 @@ via_status via_paged_append(const via_paged *c, int32_t slot, const void *qkv, i
  *             [rows]: a row sees the positions before the batch's, and position
  *             kv_len - n + o (o < min(n, VIA_MAX_TREE_ROWS)) iff bit o of its mask
  *             is set (a token tree; give no window, EINVAL).
- *   out       [rows][out_ld], written; a row that sees nothing gets zeros
+ *   out       [rows][out_ld], written; a row that sees nothing gets zeros.  May be q
+ *             itself with out_ld == q_ld, and overlap it in no other way (EINVAL is
+ *             for the same address with another length only)
  *   lse       fp32 [rows][n_heads] or NULL: log of the sum of exp(scale q K^T), -inf
  *             for a row that sees nothing
  *   workspace device, 256-byte aligned, >= via_paged_attend_bytes (ENOMEM; may be
  *             NULL where that is 0)
  * scale > 0.  A key that a row does not see adds nothing to it, whatever its page
- * holds.  Scores, softmax and sums are fp32. */
+ * holds.  Scores, softmax and sums are fp32; a bf16 call of 128 queries (rows times
+ * heads of a K/V head) a sequence or more, on average, rounds the softmax's weights to
+ * bf16 for their products with V, others keep 16 bits of them or more. */
 size_t via_paged_attend_bytes(const via_paged *c, int32_t n_heads, int32_t window);
 via_status via_paged_attend(const via_paged *c, int32_t slot, const void *q, int32_t q_ld, int32_t n_heads, float scale,
                             int32_t window, const uint64_t *row_mask, void *out, int32_t out_ld, float *lse,
@@ -348,7 +353,8 @@ via_status via_paged_block_means(const via_paged *c, int32_t slot, int32_t block
  *   sel    device [rows][n_kv_heads][n_sel], written: ascending blocks, then -1
  *          where the row sees fewer
  *   workspace device, 256-byte aligned, >= via_paged_select_bytes (ENOMEM)
- * n_first + n_last <= n_sel.  The pool and the table are not read. */
+ * n_first + n_last <= n_sel.  The pool and the table are given as for the other
+ * calls and not read. */
 size_t via_paged_select_bytes(const via_paged *c, int32_t block);
 via_status via_paged_select(const via_paged *c, const void *q, int32_t q_ld, int32_t n_heads, const float *means,
                             int32_t max_blocks, int32_t block, int32_t n_first, int32_t n_last, int32_t n_sel,

@@ -17,7 +17,6 @@ constexpr int kMaxPositions = 1 << 30;  // cache positions of a sequence
 constexpr int kMaxSeqs = 65535;         // a grid's extent
 constexpr int kMaxRows = 1 << 27;       // of a call
 constexpr long long kMaxGroups = 1 << 24;  // work-groups of 256 threads in a launch (2^32 threads)
-constexpr int kMaxBlocks = 65535 * 128;     // blocks of a sequence that a choice is made of
 constexpr int kMaxSplits = 64;
 
 int esize(const via_paged* c) { return c->dtype == VIA_DTYPE_BF16 ? 2 : 4; }
@@ -170,7 +169,8 @@ via_status check_attention(const via_paged* c, int slot, const void* q, int q_ld
   if (!std::isnormal(scale) || !(scale > 0.f)) return fail(VIA_EINVAL, "scale must be positive and finite");
   if (c->rows == 0 || c->n_seqs == 0) return VIA_OK;
   if (via_status st = check_rows(c, "q", q, q_ld, n_heads)) return st;
-  return check_rows(c, "out", out, out_ld, n_heads);
+  if (via_status st = check_rows(c, "out", out, out_ld, n_heads)) return st;
+  return out == q && out_ld != q_ld ? fail(VIA_EINVAL, "out over q must have its row length") : VIA_OK;
 }
 
 }  // namespace
@@ -265,9 +265,8 @@ via_status via_paged_select(const via_paged* c, const void* q, int32_t q_ld, int
   if (!block_ok(block)) return fail(VIA_EUNSUPPORTED, "blocks of %d tokens (32, 64 and 128 run)", block);
   if (n_first < 0 || n_last < 1 || n_sel < 1 || (long long)n_first + n_last > n_sel)
     return fail(VIA_EINVAL, "need n_first >= 0, n_last >= 1 and n_first + n_last <= n_sel");
-  if ((long long)c->rows * c->n_kv_heads >= kMaxGroups || ceil_div(cap_of(c), block) > kMaxBlocks)
-    return fail(VIA_EUNSUPPORTED, "%d rows of %d K/V heads and %d positions are more than a launch covers", c->rows,
-                c->n_kv_heads, cap_of(c));
+  if ((long long)c->rows * c->n_kv_heads >= kMaxGroups)
+    return fail(VIA_EUNSUPPORTED, "%d rows of %d K/V heads are more than one launch covers", c->rows, c->n_kv_heads);
   const int nb = ceil_div(cap_of(c), block);
   if (max_blocks < 1 || max_blocks < nb) return fail(VIA_EINVAL, "means of %d blocks, sequences of %d", max_blocks, nb);
   if (c->rows == 0 || c->n_seqs == 0) return VIA_OK;

@@ -19,7 +19,7 @@
 //     (m/16)*16 + ((m/4)%2)*8 + ((m/8)%2)*4 + m%4, so register i of lane l holds
 //     key (i/8)*16 + (l/32)*8 + i%8: eight consecutive keys, a V page's 16 bytes.
 //     P is split in two bf16 terms (16 bits): the loop waits for memory, and one
-//     term would double the rounding error of the output.
+//     term would add about as much error again as the output's rounding has.
 //   fp32, v_mfma_f32_32x32x2_f32: register i holds key (i/4)*8 + (l/32)*4 + i%4,
 //     four consecutive tokens of a V page a lane.  The contraction over the head
 //     dimension takes dims j and j + 4 of a group of eight in one instruction.

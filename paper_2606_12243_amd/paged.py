@@ -18,7 +18,8 @@ chosen blocks only::
 The page table, row starts and lengths stay on the device and are read by the
 kernels, so a captured HIP graph follows them from replay to replay.  Calls run on
 the current stream of the cache's device.  Rows behind the last sequence keep
-what the output held (an output the call allocates holds nothing there).
+what the output held (an output the call allocates holds nothing there).  They are for
+inference: none has a gradient.
 """
 from __future__ import annotations
 
@@ -113,6 +114,8 @@ class PagedBatch:
         hd, shape, stride = self.cache.head_dim, t.shape, t.stride()
         if t.dtype != self.cache.dtype or t.device != self.cache.device:
             raise ValueError(f"{what} must be {self.cache.dtype} on {self.cache.device}, as the pool is")
+        if t.requires_grad:
+            raise ValueError(f"{what} requires a gradient; the operators have none (call them under torch.no_grad)")
         if len(shape) == 3:
             ok = shape[1] == heads and shape[2] == hd and stride[2] == 1 and (heads == 1 or stride[1] == hd)
         else:
@@ -153,9 +156,11 @@ class PagedBatch:
         src, ld = self._rows_of(qkv, n_heads + 2 * self.cache.n_kv_heads, "qkv")
         if out is None:
             out = torch.empty((self.rows, n_heads, hd), dtype=qkv.dtype, device=qkv.device)
-        dst, out_ld = self._rows_of(out, n_heads, "out")
-        if dst == src:
-            out_ld = ld
+            dst, out_ld = out.data_ptr(), n_heads * hd
+        else:
+            dst, out_ld = self._rows_of(out, n_heads, "out")
+            if dst == src:
+                out_ld = ld
         self._call(via.via_paged_append, slot, src, ld, n_heads, self._vector(pos, torch.int32, (self.rows,), "pos"),
                    self._vector(q_gain, self.cache.dtype, (hd,), "q_gain"),
                    self._vector(k_gain, self.cache.dtype, (hd,), "k_gain"), eps, theta, dst, out_ld)
@@ -165,7 +170,9 @@ class PagedBatch:
         src, ld = self._rows_of(q, heads, "q")
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        dst, out_ld = self._rows_of(out, heads, "out")
+            dst, out_ld = out.data_ptr(), heads * self.cache.head_dim
+        else:
+            dst, out_ld = self._rows_of(out, heads, "out")
         lse = torch.empty((self.rows, heads), dtype=torch.float32, device=q.device) if return_lse else None
         ws, nbytes = self._workspace(*workspace)
         self._call(f, head_args[0], src, ld, heads, *head_args[1:], *tail_args, dst, out_ld,

@@ -573,3 +573,55 @@ def test_select_where_32_bits_do_not_decide(dtype, hd, case):
     got = on_gpu(b).select_blocks(q.cuda(), m.cuda(), n_sel, block=block, n_first=1, n_last=2)
     torch.cuda.synchronize()
     assert torch.equal(got.cpu(), ref.select(b, q, m, n_sel, block, 1, 2))
+
+
+@pytest.mark.parametrize("rows,lens", [([1, 2], [900, 40]), ([60, 5], [60, 700])])
+def test_output_over_the_queries(rows, lens):
+    say("in place", rows, lens)
+    b = ref.Batch(BF16, 8, 2, 128, rows, lens, seed=3)
+    q = b.randn(b.T, 8, 128).to(BF16)
+    step = on_gpu(b)
+    sel = torch.arange(3, dtype=torch.int32, device="cuda").expand(b.T, 2, 3).contiguous()
+    for f in (lambda t, o: step.attend(b.slot, t, out=o), lambda t, o: step.attend_blocks(b.slot, t, sel, block=32, out=o)):
+        apart = f(q.cuda(), None)
+        t = q.cuda()
+        f(t, t)
+        torch.cuda.synchronize()
+        assert torch.equal(t, apart)
+
+
+def test_binding_refuses():
+    b = ref.Batch(BF16, 4, 2, 64, [3], [40], seed=1)
+    step = on_gpu(b)
+    q = b.randn(b.T, 4, 64).to(BF16).cuda()
+    means = torch.zeros(1, 2, 3, 64, device="cuda")
+    sel = torch.zeros(3, 2, 2, dtype=torch.int32, device="cuda")
+    bad = [
+        lambda: step.attend(1, q.float()), lambda: step.attend(1, q.cpu()), lambda: step.attend(1, q[:2]),
+        lambda: step.attend(1, q[:, :, :32]), lambda: step.attend(1, q.transpose(1, 2)),
+        lambda: step.attend(1, q.clone().requires_grad_()), lambda: step.attend(1, q, out=q[:, :2]),
+        lambda: step.attend(1, q, row_mask=torch.zeros(3, dtype=torch.int32, device="cuda")),
+        lambda: step.append(1, q, 4), lambda: step.append(1, q.reshape(3, 256), 2, pos=torch.zeros(2, dtype=torch.int32, device="cuda")),
+        lambda: step.append(1, q.new_zeros(3, 512), 4, q_gain=q.new_zeros(32)),
+        lambda: step.block_means(1, means.double()), lambda: step.block_means(1, means[:, :1]),
+        lambda: step.select_blocks(q, means[0], 4), lambda: step.select_blocks(q, means, 4, out=sel),
+        lambda: step.attend_blocks(1, q, sel.long()), lambda: step.attend_blocks(1, q, sel[:2]),
+        lambda: paged.PagedBatch(step.cache, step.row_start, step.kv_len.long(), 3, 40),
+        lambda: paged.PagedBatch(step.cache, step.kv_len, step.kv_len, 3, 40),
+        lambda: paged.PagedCache(step.cache.pool, 2, 64, step.table.cpu()),
+        lambda: paged.PagedCache(step.cache.pool, 3, 64, step.table),
+        lambda: paged.PagedCache(step.cache.pool[..., ::2], 2, 64, step.table),
+    ]
+    for i, f in enumerate(bad):
+        with pytest.raises(ValueError):
+            f()
+            pytest.fail(f"call {i} was not refused")
+    for f in (lambda: step.attend(2, q), lambda: step.attend(1, q, scale=0.0), lambda: step.attend(1, q, window=-1),
+              lambda: step.attend_blocks(1, q, sel, block=48), lambda: step.select_blocks(q, means[:, :, :1].contiguous(), 4, block=32)):
+        with pytest.raises(via.ViaError):
+            f()
+    # part of a wider table, at its end
+    wide = torch.full((1, 9), -1, dtype=torch.int32, device="cuda")
+    wide[:, 5:8] = step.table[:, :3]
+    part = paged.PagedBatch(paged.PagedCache(step.cache.pool, 2, 64, wide[:, 5:8]), step.row_start, step.kv_len, 3, 1000)
+    assert torch.equal(part.attend(1, q), step.attend(1, q))

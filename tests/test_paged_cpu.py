@@ -65,6 +65,7 @@ def test_bad_batches(op, bad, status):
         (["attend", "select", "blocks"], dict(q_ld=248), via.EINVAL), (["attend", "select", "blocks"], dict(q_ld=257), via.EINVAL),
         (["append", "attend", "blocks"], dict(out=None), via.EINVAL), (["append", "attend", "blocks"], dict(out=A + 8), via.EINVAL),
         (["append", "attend", "blocks"], dict(out_ld=128), via.EINVAL),
+        (["attend", "blocks"], dict(out=A, q=A, out_ld=264), via.EINVAL),
         (["attend", "blocks"], dict(scale=0.0), via.EINVAL), (["attend", "blocks"], dict(scale=-1.0), via.EINVAL),
         (["attend", "blocks"], dict(scale=math.nan), via.EINVAL), (["attend", "blocks"], dict(scale=math.inf), via.EINVAL),
         (["attend", "blocks"], dict(scale=1e-42), via.EINVAL),
@@ -112,6 +113,8 @@ def test_a_launch_has_an_end():
     d = desc(rows=2 ** 31 - 1, n_seqs=1, table_ld=4, max_kv=60)
     assert call("attend", d) == via.EUNSUPPORTED
     assert call("blocks", d) == via.EUNSUPPORTED
+    for op in ("attend", "select", "blocks"):
+        assert call(op, desc(rows=1 << 24, n_seqs=1)) == via.EUNSUPPORTED, op
 
 
 def test_binding_refuses_what_it_cannot_pass():
