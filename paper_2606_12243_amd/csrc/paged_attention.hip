@@ -549,7 +549,7 @@ __global__ __launch_bounds__(256, (sizeof(T) * HD <= 256 ? 2 : 1)) void paged_st
 // operands.  Pages are copied as they are, but that the two 16-byte halves of a V
 // row go apart, so that every operand read is 256 consecutive bytes per 16 lanes.
 // Two work-groups share a compute unit: one's softmax runs beside the other's
-// products.  The weights are one bf16 value each (TERMS = 1, to nearest: 2^-9 of
+// products.  The weights are one bf16 value each (TERMS = 1, to nearest: 2^-8 of
 // a weight at most, about what the output's own rounding costs, where two would be
 // half again the products), or two where few rows leave the loop waiting for
 // memory.  The running maximum is raised only when it grows by more than 2^8,
@@ -668,11 +668,22 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
       __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
       settle();
       if (!all) {
+        if (absent || a.row_mask) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const uint32_t seen = seen_keys<uint16_t>(q, kb + b * 32, !((absent >> (2 * b)) & 1), !((absent >> (2 * b + 1)) & 1), half);
+          for (int b = 0; b < 2; ++b) {
+            const uint32_t seen =
+                seen_keys<uint16_t>(q, kb + b * 32, !((absent >> (2 * b)) & 1), !((absent >> (2 * b + 1)) & 1), half);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s[b][i] = (seen >> i) & 1 ? s[b][i] : -INFINITY;
+            for (int i = 0; i < 16; ++i) s[b][i] = (seen >> i) & 1 ? s[b][i] : -INFINITY;
+          }
+        } else {  // keys lo .. vis - 1: a comparison a score
+          const int lo = q.lo - kb - half * 8;
+          const uint32_t n_seen = q.valid ? max(q.vis - q.lo, 0) : 0;
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              s[b][i] = (uint32_t)(b * 32 + (i >> 3) * 16 + (i & 7) - lo) < n_seen ? s[b][i] : -INFINITY;
         }
       }
       // (maximum, not fmaxf: one instruction for two values, NaN kept)
@@ -695,7 +706,6 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
       const float neg_m = acc.m == -INFINITY ? 0.f : -acc.m;
       // half a tile's weights and values at a time: the second half's weights run beside the first half's products
       uint4 v[2][2 * DT], p[2][2], p2[2][2];
-      uint32_t bits = 0;
       auto values = [&](int b) {
 #pragma unroll
         for (int i = 0; i < 2 * DT; ++i) v[b][i] = *(const uint4*)(sv + (b * 2 + i / DT) * kPage + i % DT * 1024);
@@ -727,11 +737,19 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
       };
       auto clean = [&](int b) {
         if (!all) {
+          uint32_t bits = 0;
 #pragma unroll
           for (int i = 0; i < 2 * DT; ++i) {
-            uint4& x = v[b][i];
+            const uint4& x = v[b][i];
             bits |= odd_bits<uint16_t>(x.x) | odd_bits<uint16_t>(x.y) | odd_bits<uint16_t>(x.z) | odd_bits<uint16_t>(x.w);
-            x = make_uint4(drop_odd<uint16_t>(x.x), drop_odd<uint16_t>(x.y), drop_odd<uint16_t>(x.z), drop_odd<uint16_t>(x.w));
+          }
+          if (__any(bits != 0)) {
+            any_odd = true;
+#pragma unroll
+            for (int i = 0; i < 2 * DT; ++i) {
+              uint4& x = v[b][i];
+              x = make_uint4(drop_odd<uint16_t>(x.x), drop_odd<uint16_t>(x.y), drop_odd<uint16_t>(x.z), drop_odd<uint16_t>(x.w));
+            }
           }
         }
       };
@@ -743,7 +761,6 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
       weights(1);
       clean(1);
       products(1);
-      any_odd |= __any(bits != 0);
     }
     pages = pages1;
     pages1 = pages2;
