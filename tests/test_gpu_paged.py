@@ -56,7 +56,8 @@ def check_attention(b, q, got, lse, n, scale, p_bits=None, **kw):
     assert (got.cpu()[live][none[live]] == 0).all()
 
 
-SHAPES = [(BF16, 8, 2, 128), (BF16, 4, 2, 64), (BF16, 3, 3, 128), (BF16, 12, 1, 64), (F32, 4, 4, 64), (F32, 6, 2, 128)]
+SHAPES = [(BF16, 8, 2, 128), (BF16, 4, 2, 64), (BF16, 3, 3, 128), (BF16, 12, 1, 64), (F32, 4, 4, 64), (F32, 6, 2, 128),
+          (BF16, 3, 1, 64), (F32, 1, 1, 64), (BF16, 40, 1, 128)]
 BATCHES = [
     ([1], [1]),                           # the first token
     ([1, 1, 1], [17, 300, 64]),           # single tokens
@@ -625,3 +626,74 @@ def test_binding_refuses():
     wide[:, 5:8] = step.table[:, :3]
     part = paged.PagedBatch(paged.PagedCache(step.cache.pool, 2, 64, wide[:, 5:8]), step.row_start, step.kv_len, 3, 1000)
     assert torch.equal(part.attend(1, q), step.attend(1, q))
+
+
+@pytest.mark.parametrize("dtype,H,KVH,hd,most", [(BF16, 4, 2, 64, 3), (F32, 2, 1, 64, 2), (BF16, 8, 1, 64, 12)])
+@pytest.mark.parametrize("n_seqs", [64, 65, 131])
+def test_many_sequences(dtype, H, KVH, hd, most, n_seqs):
+    """More sequences than a wave has lanes, those without rows among them, through every operator."""
+    say("many sequences", dtype, H, KVH, hd, most, n_seqs)
+    g = torch.Generator().manual_seed(n_seqs)
+    rows = torch.randint(0, most + 1, (n_seqs,), generator=g).tolist()
+    lens = [n + int(c) for n, c in zip(rows, torch.randint(0, 90, (n_seqs,), generator=g))]
+    rows[0], lens[0], rows[-1], lens[-1], rows[63], lens[63] = 0, 0, most, 300, most, most
+    b = ref.Batch(dtype, H, KVH, hd, rows, lens, seed=most, pad=2)
+    step = on_gpu(b)
+    qkv = b.randn(b.T, (H + 2 * KVH) * hd).to(dtype)
+    q = check_append(b, step, qkv, 10000.0, 1e-5, [None, None], None)
+    b.pool = step.cache.pool.cpu()
+    out, lse = step.attend(b.slot, q, return_lse=True)
+    torch.cuda.synchronize()
+    check_attention(b, q.cpu(), out, lse, b.max_kv, hd ** -0.5)
+    old = b.randn(n_seqs, KVH, 11, hd)
+    got = step.block_means(b.slot, old.cuda(), block=32)
+    torch.cuda.synchronize()
+    want, mag = ref.means(b, old, 32)
+    assert ((got.double().cpu() - want).abs() <= 7 * 2.0 ** -24 * mag).all()
+    sel = step.select_blocks(q, got, 3, block=32)
+    torch.cuda.synchronize()
+    n = b.start[-1]
+    assert torch.equal(sel[:n].cpu(), ref.select(b, q.cpu(), got.cpu(), 3, 32, 1, 2)[:n])
+    out, lse = step.attend_blocks(b.slot, q, sel, block=32, return_lse=True)
+    torch.cuda.synchronize()
+    check_attention(b, q.cpu(), out, lse, 96, hd ** -0.5, sel=sel.cpu(), block=32)
+
+
+@pytest.mark.parametrize("dtype,H,KVH,hd,rows", [(BF16, 8, 2, 128, 1), (F32, 2, 1, 64, 3), (BF16, 8, 2, 64, 50), (BF16, 32, 1, 128, 70)])
+def test_values_outside_a_window(dtype, H, KVH, hd, rows):
+    """NaN and infinities in keys and values that the window leaves behind, inside a page and whole pages."""
+    say("outside a window", dtype, H, KVH, hd, rows)
+    window, len_ = 45, 700
+    b = ref.Batch(dtype, H, KVH, hd, [rows], [len_], seed=rows)
+    q = b.randn(b.T, H, hd).to(dtype)
+    first = len_ - rows - window + 1  # the first key of the first row
+    pool = b.pool.clone()
+    k = pool[b.slot][:, :, 0].view(KVH, b.n_blocks, hd // 8, 16, 8)
+    v = pool[b.slot][:, :, 1].view(KVH, b.n_blocks, hd, 16)
+    for pos in range(first):
+        p = b.page(0, pos)
+        k[:, p, :, pos % 16] = (math.nan, math.inf, -math.inf)[pos % 3]
+        v[:, p, :, pos % 16] = (-math.inf, math.nan, math.inf)[pos % 3]
+    clean, b.pool = b.pool, pool
+    out, lse = on_gpu(b).attend(b.slot, q.cuda(), window=window, return_lse=True)
+    torch.cuda.synchronize()
+    b.pool = clean
+    check_attention(b, q, out, lse, window + 1, hd ** -0.5, window=window)
+
+
+@pytest.mark.parametrize("dtype,H,KVH,hd,rows", [(BF16, 8, 2, 128, 2), (F32, 2, 1, 64, 2), (BF16, 4, 2, 64, 20), (BF16, 8, 2, 128, 90)])
+@pytest.mark.parametrize("grow", [0.5, 6.0, 40.0, -6.0])
+def test_scores_that_climb(dtype, H, KVH, hd, rows, grow):
+    """The running maximum moves a little, much, or never after the first keys: scores climb (or fall) by
+    ``grow`` every 64 keys, the largest ones far from zero."""
+    say("climb", dtype, H, KVH, hd, rows, grow)
+    len_ = 900
+    b = ref.Batch(dtype, H, KVH, hd, [rows], [len_], seed=rows)
+    k = b.pool[b.slot][:, :, 0].view(KVH, b.n_blocks, hd // 8, 16, 8)
+    for pos in range(len_):
+        k[:, b.page(0, pos), 0, pos % 16, 0] = pos * grow / 64
+    q = b.randn(b.T, H, hd).to(dtype)
+    q[:, :, 0] = hd ** 0.5
+    out, lse = on_gpu(b).attend(b.slot, q.cuda(), return_lse=True)
+    torch.cuda.synchronize()
+    check_attention(b, q, out, lse, b.max_kv, hd ** -0.5)
