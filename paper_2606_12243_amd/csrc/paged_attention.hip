@@ -324,13 +324,18 @@ __device__ __forceinline__ void compute_block(Block<T, HD>& b, int kb, bool page
   }
 }
 
+// First position of the window at `pos` (no difference that a window of all positions overflows).
+__device__ __forceinline__ int window_from(const PagedAttnArgs& a, int pos) {
+  return a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
+}
+
 // Queries q0 .. q0 + tile_q - 1 of a sequence: the keys [lo, end) that their rows
 // see, lo on a page-pair border.
 __device__ __forceinline__ void tile_keys(const PagedAttnArgs& a, int len, int n, int q0, int& lo, int& end) {
   const int G = a.H / a.c.KVH, pos0 = len - n;
   const int r0 = q0 / G, r1 = min(n - 1, (q0 + a.tile_q - 1) / G);
   end = min(a.row_mask ? len : pos0 + r1 + 1, a.c.cap);
-  lo = a.window > 0 ? max(0, pos0 + r0 - a.window + 1) & ~31 : 0;
+  lo = min(window_from(a, pos0 + r0), max(end, 0)) & ~31;
 }
 
 // Query qi = row * G + head of a sequence's queries under K/V head g.
@@ -340,7 +345,7 @@ __device__ __forceinline__ Query query_of(const PagedAttnArgs& a, int g, int qi,
   q.valid = r < n;
   q.row = first + min(r, n - 1);
   q.head = g * G + qi % G;
-  q.lo = a.window > 0 ? max(0, pos - a.window + 1) : 0;
+  q.lo = window_from(a, pos);
   q.vis = a.row_mask ? min(len - n, a.c.cap) : min(pos, a.c.cap - 1) + 1;
   q.base = len - n;
   q.mask = 0;

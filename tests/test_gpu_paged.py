@@ -697,3 +697,48 @@ def test_scores_that_climb(dtype, H, KVH, hd, rows, grow):
     out, lse = on_gpu(b).attend(b.slot, q.cuda(), return_lse=True)
     torch.cuda.synchronize()
     check_attention(b, q, out, lse, b.max_kv, hd ** -0.5)
+
+
+@pytest.mark.parametrize("dtype,H,KVH,hd", [(BF16, 8, 2, 128), (F32, 2, 1, 64)])
+@pytest.mark.parametrize("rows", [3, 60])
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 2, 2 ** 30])
+def test_window_of_all_positions(dtype, H, KVH, hd, rows, window):
+    """The largest windows, with rows at negative positions before them."""
+    say("largest window", dtype, rows, window)
+    b = ref.Batch(dtype, H, KVH, hd, [rows, 2], [rows - 2, 700], seed=rows)
+    q = b.randn(b.T, H, hd).to(dtype)
+    out, lse = on_gpu(b).attend(b.slot, q.cuda(), window=window, return_lse=True)
+    torch.cuda.synchronize()
+    check_attention(b, q, out, lse, b.max_kv, hd ** -0.5, window=window)
+
+
+@pytest.mark.parametrize("dtype,H,KVH,hd", [(BF16, 8, 2, 128), (F32, 2, 1, 64)])
+@pytest.mark.parametrize("rows", [3, 60])
+@pytest.mark.parametrize("window", [0, 100, 2 ** 31 - 1])
+def test_lengths_far_past_the_bound(dtype, H, KVH, hd, rows, window):
+    """A length up to 2^31 - 1 on the device: its rows cache nothing and see what max_kv leaves of their keys."""
+    say("far lengths", dtype, rows, window)
+    far = 2 ** 31 - 1
+    b = ref.Batch(dtype, H, KVH, hd, [rows, 2], [700, 40], seed=rows)
+    b.lens[0] = far
+    b.kv_len = torch.tensor(b.lens, dtype=torch.int32)
+    b.max_kv = 650
+    step = on_gpu(b)
+    q = b.randn(b.T, H, hd).to(dtype)
+    out, lse = step.attend(b.slot, q.cuda(), window=window, return_lse=True)
+    torch.cuda.synchronize()
+    check_attention(b, q, out, lse, b.max_kv, hd ** -0.5, window=window)
+    old = b.randn(2, KVH, 21, hd)
+    got = step.block_means(b.slot, old.cuda(), block=32)
+    sel = step.select_blocks(q.cuda(), got, 5, block=32)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0].cpu(), old[0])
+    assert torch.equal(sel.cpu(), ref.select(b, q, got.cpu(), 5, 32, 1, 2))
+    out, lse = step.attend_blocks(b.slot, q.cuda(), sel, block=32, return_lse=True)
+    torch.cuda.synchronize()
+    check_attention(b, q, out, lse, 160, hd ** -0.5, sel=sel.cpu(), block=32)
+    before = step.cache.pool.clone()
+    step.append(b.slot, b.randn(b.T, (H + 2 * KVH) * hd).to(dtype).cuda(), H)
+    torch.cuda.synchronize()
+    changed = (step.cache.pool != before).flatten(3).any(-1).any(1).any(0)
+    assert changed.nonzero()[:, 0].tolist() == sorted({b.page(1, 38), b.page(1, 39)})
