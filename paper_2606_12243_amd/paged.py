@@ -37,13 +37,20 @@ def _expect(cond, what):
         raise ValueError(what)
 
 
+def _int32(*values):
+    for v in values:
+        if not -(1 << 31) <= v < 1 << 31:
+            raise ValueError(f"{v} is out of range")
+
+
 class PagedCache:
     """``pool``: contiguous device tensor [n_slots, n_kv_heads, n_blocks, 2, 16 * head_dim]
     (or that many elements flat, with ``n_slots``), fp32 or bf16.  ``table``: int32 [n_seqs,
     pages] on the same device, rows contiguous; entries outside the pool name no page."""
 
     def __init__(self, pool, n_kv_heads, head_dim, table, n_slots=None):
-        _expect(pool.is_cuda and pool.is_contiguous(), "the pool must be a contiguous device tensor")
+        _expect(pool.is_cuda and pool.is_contiguous() and not pool.requires_grad,
+                "the pool must be a contiguous device tensor without a gradient")
         _expect(pool.dtype in _DTYPES, f"a pool of {pool.dtype} (float32 or bfloat16)")
         _expect(n_kv_heads >= 1 and head_dim >= 1, "n_kv_heads and head_dim must be positive")
         n_slots = n_slots if n_slots is not None else (pool.shape[0] if pool.dim() == 5 else 1)
@@ -90,6 +97,7 @@ class PagedBatch:
                     and t.is_contiguous(), f"row_start and kv_len must be int32 [{n + 1}] and [{n}] on the pool's device")
         self.cache, self.row_start, self.kv_len, self.table = cache, row_start, kv_len, cache.table
         # (a table that is part of a wider one: no more than its own columns)
+        _int32(rows, cache.n_blocks, cache.n_slots, self.table.stride(0))
         self.rows, self.max_kv, self.n_seqs = int(rows), min(int(max_kv), self.table.shape[1] * via.BLOCK), n
         self.c = via.Paged(cache.pool.data_ptr(), _DTYPES[cache.dtype], cache.n_slots, cache.n_blocks, cache.n_kv_heads,
                            cache.head_dim, self.table.data_ptr(), max(1, self.table.stride(0)), n, row_start.data_ptr(),
@@ -114,7 +122,7 @@ class PagedBatch:
         hd, shape, stride = self.cache.head_dim, t.shape, t.stride()
         if t.dtype != self.cache.dtype or t.device != self.cache.device:
             raise ValueError(f"{what} must be {self.cache.dtype} on {self.cache.device}, as the pool is")
-        if t.requires_grad:
+        if t.requires_grad and torch.is_grad_enabled():
             raise ValueError(f"{what} requires a gradient; the operators have none (call them under torch.no_grad)")
         if len(shape) == 3:
             ok = shape[1] == heads and shape[2] == hd and stride[2] == 1 and (heads == 1 or stride[1] == hd)
@@ -122,7 +130,10 @@ class PagedBatch:
             ok = len(shape) == 2 and shape[1] == heads * hd and stride[1] == 1
         if not ok or shape[0] != self.rows:
             raise ValueError(f"{what} of shape {tuple(shape)}: {self.rows} rows of {heads} heads of {hd}, a row contiguous")
-        return t.data_ptr(), (stride[0] if self.rows > 1 else heads * hd)
+        ld = stride[0] if self.rows > 1 else heads * hd
+        if ld >= 1 << 31:
+            raise ValueError(f"{what}: rows {ld} elements apart (less than 2^31)")
+        return t.data_ptr(), ld
 
     def _heads_of(self, q):
         hd = self.cache.head_dim
@@ -135,7 +146,20 @@ class PagedBatch:
             return None
         if t.dtype != dtype or t.device != self.cache.device or t.shape != shape or not t.is_contiguous():
             raise ValueError(f"{what} must be contiguous {dtype} {list(shape)} on {self.cache.device}")
+        if t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{what} requires a gradient; the operators have none (call them under torch.no_grad)")
         return t.data_ptr()
+
+    def _apart(self, src, ld, heads, dst, out_ld, out_heads):
+        """Refuses an output that lies over its input but in its own place (the same start and rows)."""
+        n, size, hd = self.rows, self.cache.pool.element_size(), self.cache.head_dim
+        if n == 0 or (dst == src and (out_ld == ld or n == 1)):
+            return
+        w, out_w = heads * hd, out_heads * hd
+        if dst >= src + ((n - 1) * ld + w) * size or src >= dst + ((n - 1) * out_ld + out_w) * size:
+            return
+        at = (dst - src) // size % ld  # side by side in the same rows
+        _expect(out_ld == ld and at >= w and at + out_w <= ld, "out overlaps the input")
 
     def _workspace(self, f, *args):
         """A workspace (None if none is needed) and its size.  It is the call's own: two calls in flight
@@ -152,6 +176,7 @@ class PagedBatch:
         queries [rows, n_heads, head_dim].  ``qkv`` [rows, (n_heads + 2 n_kv_heads) * head_dim];
         ``pos`` int32 [rows]: rotary positions other than the cache's; ``out``: where the queries
         go, qkv[:, :n_heads * head_dim] among others."""
+        _int32(slot, n_heads)
         hd = self.cache.head_dim
         src, ld = self._rows_of(qkv, n_heads + 2 * self.cache.n_kv_heads, "qkv")
         if out is None:
@@ -159,7 +184,8 @@ class PagedBatch:
             dst, out_ld = out.data_ptr(), n_heads * hd
         else:
             dst, out_ld = self._rows_of(out, n_heads, "out")
-            if dst == src:
+            self._apart(src, ld, n_heads + 2 * self.cache.n_kv_heads, dst, out_ld, n_heads)
+            if dst == src and self.rows == 1:
                 out_ld = ld
         self._call(via.via_paged_append, slot, src, ld, n_heads, self._vector(pos, torch.int32, (self.rows,), "pos"),
                    self._vector(q_gain, self.cache.dtype, (hd,), "q_gain"),
@@ -173,6 +199,7 @@ class PagedBatch:
             dst, out_ld = out.data_ptr(), heads * self.cache.head_dim
         else:
             dst, out_ld = self._rows_of(out, heads, "out")
+            self._apart(src, ld, heads, dst, out_ld, heads)
         lse = torch.empty((self.rows, heads), dtype=torch.float32, device=q.device) if return_lse else None
         ws, nbytes = self._workspace(*workspace)
         self._call(f, head_args[0], src, ld, heads, *head_args[1:], *tail_args, dst, out_ld,
@@ -183,6 +210,7 @@ class PagedBatch:
         """Attention of the rows over their cached sequences: causal, the last ``window`` positions
         (0: all), or with ``row_mask`` (int64 [rows], bit o: the batch's own position o) a token
         tree.  ``scale`` defaults to head_dim ** -0.5."""
+        _int32(slot, window)
         heads = self._heads_of(q)
         mask = self._vector(row_mask, torch.int64, (self.rows,), "row_mask")
         scale = self.cache.head_dim ** -0.5 if scale is None else scale
@@ -192,6 +220,7 @@ class PagedBatch:
     def block_means(self, slot, means, block=64):
         """Mean keys of the blocks the rows complete, into ``means`` (fp32 [n_seqs, n_kv_heads,
         blocks, head_dim]); returns it."""
+        _int32(slot, block)
         n = means.shape[2] if means.dim() == 4 else 0
         addr = self._vector(means, torch.float32, (self.n_seqs, self.cache.n_kv_heads, n, self.cache.head_dim), "means")
         self._call(via.via_paged_block_means, slot, block, addr, n)
@@ -199,6 +228,7 @@ class PagedBatch:
 
     def select_blocks(self, q, means, n_sel, block=64, n_first=1, n_last=2, out=None):
         """The blocks each row reads: int32 [rows, n_kv_heads, n_sel], ascending, then -1."""
+        _int32(n_sel, block, n_first, n_last)
         heads, kvh = self._heads_of(q), self.cache.n_kv_heads
         src, ld = self._rows_of(q, heads, "q")
         n = means.shape[2] if means.dim() == 4 else 0
@@ -213,6 +243,7 @@ class PagedBatch:
 
     def attend_blocks(self, slot, q, sel, block=64, scale=None, out=None, return_lse=False):
         """``attend`` over the blocks listed in ``sel`` (int32 [rows, n_kv_heads, n_sel])."""
+        _int32(slot, block)
         heads = self._heads_of(q)
         n_sel = sel.shape[2] if sel.dim() == 3 else 0
         lists = self._vector(sel, torch.int32, (self.rows, self.cache.n_kv_heads, n_sel), "sel")

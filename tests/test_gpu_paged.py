@@ -742,3 +742,37 @@ def test_lengths_far_past_the_bound(dtype, H, KVH, hd, rows, window):
     torch.cuda.synchronize()
     changed = (step.cache.pool != before).flatten(3).any(-1).any(1).any(0)
     assert changed.nonzero()[:, 0].tolist() == sorted({b.page(1, 38), b.page(1, 39)})
+
+
+def test_binding_refuses_overlaps_gradients_and_numbers_out_of_range():
+    b = ref.Batch(BF16, 4, 2, 64, [3], [40], seed=1)
+    step = on_gpu(b)
+    flat = torch.zeros(4000, dtype=BF16, device="cuda")
+    qkv = flat[:3 * 600].view(3, 600)[:, :512]
+    q = qkv[:, :256]
+    gain = torch.nn.Parameter(torch.ones(64, dtype=BF16, device="cuda"))
+    sel = torch.zeros(3, 2, 2, dtype=torch.int32, device="cuda")
+    means = torch.zeros(1, 2, 2, 64, device="cuda")
+    bad = [
+        lambda: step.append(1, qkv, 4, out=flat[:768].view(3, 256)),  # the same start, other rows
+        lambda: step.append(1, qkv, 4, out=qkv[:, 8:264]), lambda: step.append(1, qkv, 4, out=qkv[:, 256:]),
+        lambda: step.append(1, qkv, 4, out=flat[600:].narrow(0, 0, 1800).view(3, 600)[:, :256]),
+        lambda: step.append(1, qkv, 4, q_gain=gain), lambda: step.append(1 << 32, qkv, 4),
+        lambda: step.attend(1, q, out=qkv[:, 128:384]), lambda: step.attend(1, q, out=flat[:768].view(3, 256)),
+        lambda: step.attend(1, q, window=1 << 32), lambda: step.attend_blocks(1, q, sel, block=(1 << 32) + 32),
+        lambda: step.attend_blocks(1, q, sel, block=32, out=qkv[:, 8:264]),
+        lambda: step.select_blocks(q, means, 4, block=32, n_first=1 << 32),
+        lambda: step.block_means(1, means, block=(1 << 32) + 32),
+        lambda: paged.PagedBatch(step.cache, step.row_start, step.kv_len, (1 << 32) + 3, 40),
+        lambda: paged.PagedCache(step.cache.pool.clone().requires_grad_(), 2, 64, step.table),
+    ]
+    for i, f in enumerate(bad):
+        with pytest.raises(ValueError):
+            f()
+            pytest.fail(f"call {i} was not refused")
+    with torch.no_grad():
+        step.append(1, qkv, 4, q_gain=gain)
+    # side by side in the same rows, and behind each other, are apart
+    want = step.attend(1, q)
+    assert torch.equal(step.attend(1, q, out=qkv[:, 256:]), want)
+    assert torch.equal(step.attend(1, q, out=flat[1800:].narrow(0, 0, 768).view(3, 256)), want)
