@@ -246,8 +246,7 @@ via_status via_paged_block_means(const via_paged* c, int32_t slot, int32_t block
   a.block = block;
   a.means = means;
   a.max_blocks = max_blocks;
-  a.per_seq = std::min({c->rows / block + 1, a.c.cap / block, max_blocks});
-  if (a.per_seq == 0) return VIA_OK;  // no sequence is long enough to complete a block
+  if (a.c.cap < block) return VIA_OK;  // no sequence is long enough to complete a block
   launch_paged_means(c->dtype == VIA_DTYPE_BF16, a, (hipStream_t)stream);
   return launched("block means");
 }

@@ -70,7 +70,6 @@ struct MeansArgs {
   int hd, block;
   float* means;  // [n_seqs][KVH][max_blocks][hd]
   int max_blocks;
-  int per_seq;  // blocks a sequence can complete in one call
 };
 
 struct SelectArgs {
@@ -99,44 +98,47 @@ __device__ __forceinline__ void seq_rows(const PagedRef& c, int s, int& first, i
 
 __device__ __forceinline__ int seq_len(const PagedRef& c, int s) { return max(c.kv_len[s], 0); }
 
-// The sequence of row t (uniform over the wave): lanes look at 64 sequences at
-// a time.  -1: no sequence has it.
-__device__ __forceinline__ int seq_of_row(const PagedRef& c, int t) {
+// The last sequence whose number base(s) is not above `item` (both uniform over the
+// wave, base ascending), -1 if none: lanes look at 64 sequences over the whole range,
+// then at those between two of them.  (Sequence after sequence, 64 at a time, took 0.8 us
+// for every 64: with 1024 of them, 13 us at the start of every work-group.)
+template <typename F>
+__device__ __forceinline__ int last_seq(const PagedRef& c, int item, F base) {
   const int lane = threadIdx.x & 63;
-  for (int s0 = 0; s0 < c.n_seqs; s0 += 64) {
-    int first = 0, n = 0;
-    if (s0 + lane < c.n_seqs) seq_rows(c, s0 + lane, first, n);
-    const uint64_t m = __ballot(t >= first && t - first < n);
-    if (m) return s0 + __ffsll((unsigned long long)m) - 1;
+  int lo = 0, span = c.n_seqs;
+  for (;;) {
+    const int stride = (span + 63) >> 6;
+    const uint64_t m = __ballot(lane * stride < span && base(lo + lane * stride) <= item);
+    if (!m) return -1;
+    const int at = (63 - __clzll((long long)m)) * stride;
+    lo += at;
+    if (stride <= 1) return lo;
+    span = min(stride, span - at);
   }
-  return -1;
+}
+__device__ __forceinline__ int first_row(const PagedRef& c, int s) { return min(max(c.row_start[s], 0), c.rows); }
+
+// The sequence of row t (uniform over the wave).  -1: no sequence has it.
+__device__ __forceinline__ int seq_of_row(const PagedRef& c, int t) {
+  const int s = last_seq(c, t, [&](int i) { return first_row(c, i); });
+  if (s < 0) return -1;
+  int first, n;
+  seq_rows(c, s, first, n);
+  return t - first < n ? s : -1;
 }
 
-// Tile `item` (uniform over the wave) when sequence after sequence is cut into
-// tiles of `per` units, `units` units a row: its sequence and number there.
-// Returns false past the last tile.
-__device__ __forceinline__ bool tile_of_item(const PagedRef& c, int item, int units, int per, int& seq, int& tile) {
-  const int lane = threadIdx.x & 63;
-  for (int s0 = 0; s0 < c.n_seqs; s0 += 64) {
-    int first = 0, n = 0;
-    if (s0 + lane < c.n_seqs) seq_rows(c, s0 + lane, first, n);
-    const int tiles = (int)(((long long)n * units + per - 1) / per);
-    int end = tiles;  // tiles of this and the lower lanes' sequences
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(end, o, 64);
-      if (lane >= o) end += v;
-    }
-    const uint64_t m = __ballot(item < end);
-    if (m) {
-      const int l = __ffsll((unsigned long long)m) - 1;
-      seq = s0 + l;
-      tile = item - (__builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(tiles, l));
-      return true;
-    }
-    item -= __builtin_amdgcn_readlane(end, 63);
-  }
-  return false;
+// Work items are numbered so that a sequence's first one is known from its first row
+// alone: sequence s with rows [first, first + n) has items from first * units / per +
+// extra * s on.  With `extra` 1 that is room for ceil(n * units / per) of them, or for the
+// blocks of `per` rows that end among n (units 1); a launch covers rows * units / per +
+// extra * n_seqs, and an item past what its sequence has does nothing.  rows * units is
+// below 2^31.  Returns false where no sequence has the item.
+__device__ __forceinline__ bool item_of(const PagedRef& c, int item, int units, int per, int extra, int& seq, int& no) {
+  auto base = [&](int s) { return first_row(c, s) * units / per + extra * s; };
+  seq = last_seq(c, item, base);
+  if (seq < 0) return false;
+  no = __builtin_amdgcn_readfirstlane(item - base(seq));
+  return true;
 }
 
 // seq_rows and seq_len of a sequence that is the same in all lanes, as scalars.

@@ -15,11 +15,13 @@ namespace {
 // v as it is.  Bound by memory: a value is read and written once.
 //
 // A work-group takes the rows that enter one page of a sequence (at most 16) and
-// some of their heads, q, k and v in one list.  Thread t holds 8 dims of the page's
-// token t / 16 (16 lanes a token: a head of 128, or two of 64), so a head's sum of
+// some of their heads, q, k and v in one list.  A team of 16 lanes holds a token's
+// head of 128 (or two of 64), 8 dims a lane, so a head's sum of
 // squares and a dim's partner are lane exchanges, and q and k go out 16 bytes a
-// thread or more.  V, transposed in its page, goes through LDS and out as 8 tokens
-// of a dim a thread, a whole page's in one piece.
+// thread or more.  More than 8 rows have a team for each of the page's tokens, and V,
+// transposed in its page, goes through LDS and out as 8 tokens of a dim a thread, a
+// whole page's in one piece.  Where fewer rows enter, as in single-token steps, the
+// teams share out the heads instead.
 //
 // Angles are whole turns in fp64, pos * (theta^(-2i/hd) / 2 pi), of which only the
 // fraction is kept: fp32 would lose it at far positions (2^-24 of 10^5 turns).
@@ -42,34 +44,39 @@ __device__ __forceinline__ float head_sum(float x) {
   return TPH == 16 ? x + ror8(x) : x;
 }
 
-// Page `item` (uniform) when the pages that each sequence's rows enter are counted
-// one sequence after another: its sequence and position / 16.  Positions
-// below 0 count as pages too (their rows only have queries).
+// Page `item` (uniform over the wave) of those that the sequences' rows enter, at most n / 16
+// + 2 of n rows: its sequence and position / 16 (pages of positions below 0 included: their
+// rows only have queries).  Up to 64 sequences' pages are counted one after another,
+// which leaves no items without work in between: with them some compute units get more
+// work-groups than others (16 prompts of 500 rows 55 against 47 us).  More are
+// searched (1024 single tokens 19 against 51 us with counting); a page behind the last one has no
+// work.
 __device__ __forceinline__ bool page_of_item(const PagedRef& c, int item, int& seq, int& page) {
-  const int lane = threadIdx.x & 63;
-  for (int s0 = 0; s0 < c.n_seqs; s0 += 64) {
-    int first = 0, n = 0, len = 0;
-    if (s0 + lane < c.n_seqs) {
-      seq_rows(c, s0 + lane, first, n);
-      len = seq_len(c, s0 + lane);
-    }
-    const int p0 = (len - n) >> 4, pages = n > 0 ? ((len - 1) >> 4) - p0 + 1 : 0;
-    int end = pages;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(end, o, 64);
-      if (lane >= o) end += v;
-    }
-    const uint64_t m = __ballot(item < end);
-    if (m) {
-      const int l = __ffsll((unsigned long long)m) - 1;
-      seq = s0 + l;
-      page = __builtin_amdgcn_readlane(p0, l) + item - (__builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(pages, l));
-      return true;
-    }
-    item -= __builtin_amdgcn_readlane(end, 63);
+  if (c.n_seqs > 64) {
+    if (!item_of(c, item, 1, 16, 2, seq, page)) return false;
+    int first, n, len;
+    seq_of_wave(c, seq, first, n, len);
+    page += (len - n) >> 4;
+    return true;
   }
-  return false;
+  const int lane = threadIdx.x & 63;
+  int first = 0, n = 0, len = 0;
+  if (lane < c.n_seqs) {
+    seq_rows(c, lane, first, n);
+    len = seq_len(c, lane);
+  }
+  const int p0 = (len - n) >> 4, pages = n > 0 ? ((len - 1) >> 4) - p0 + 1 : 0;
+  int end = pages;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(end, o, 64);
+    if (lane >= o) end += v;
+  }
+  const uint64_t m = __ballot(item < end);
+  if (!m) return false;
+  seq = __ffsll((unsigned long long)m) - 1;
+  page = __builtin_amdgcn_readlane(p0, seq) + item - (__builtin_amdgcn_readlane(end, seq) - __builtin_amdgcn_readlane(pages, seq));
+  return true;
 }
 
 // 8 values as floats, and back
@@ -110,25 +117,36 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
   constexpr int kVec = 16 / sizeof(T);                        // tokens of a dim a thread stores
   constexpr int kStride = 16 + kVec;                          // of a dim in LDS (no bank conflicts on reading)
   __shared__ __align__(16) T vt[HPP * HD * kStride];
-  const int l = threadIdx.x & 15, sub = l / TPH, d0 = (l % TPH) * 8, t = threadIdx.x >> 4;
+  const int l = threadIdx.x & 15, d0 = (l % TPH) * 8, team = threadIdx.x >> 4;
   int seq, page_no, first, n, len;
   if (!page_of_item(a.c, blockIdx.x, seq, page_no)) return;
   seq_of_wave(a.c, seq, first, n, len);
-  const int slot0 = page_no * 16, r = slot0 + t - (len - n);  // the thread's row of the sequence
-  const bool live = r >= 0 && r < n;
-  const int row = first + min(max(r, 0), n - 1);
-  const bool cached = slot0 >= 0 && slot0 + t < a.c.cap;
+  if (n == 0 || page_no > (len - 1) >> 4) return;
+  const int slot0 = page_no * 16;
+  // the page's tokens t0 .. t1 - 1 are rows of the call: `rows` teams take them (or the whole page), the others
+  // further heads
+  const int t0 = max(len - n - slot0, 0), t1 = min(len - slot0, 16);
+  const int bits = t1 - t0 > 8 ? 4 : t1 - t0 > 4 ? 3 : t1 - t0 > 2 ? 2 : t1 - t0 - 1, rows = 1 << bits;
+  const int t = (rows == 16 ? 0 : t0) + (team & (rows - 1)), sub = (team >> bits) * HPP + l / TPH;
+  const bool live = t >= t0 && t < t1;
+  const int pos0 = slot0 + min(max(t, t0), t1 - 1), row = first + pos0 - (len - n);  // the thread's position and row
+  const bool cached = slot0 >= 0 && pos0 < a.c.cap;
   const int page = slot0 >= 0 ? __builtin_amdgcn_readfirstlane(page_of(a.c, seq, page_no)) : -1;
-  const int heads = a.H + 2 * a.c.KVH;
+  const int heads = a.H + 2 * a.c.KVH, width = HPP * 16 >> bits;  // heads a pass takes
+  // the work-group's passes y, y + gridDim.y, ..., from another one in every work-group: rows whose length is a
+  // multiple of 4 KiB would have all of them read the same memory channels
+  const int passes = ((heads + width - 1) / HPP >> (4 - bits)) - (int)blockIdx.y;
+  const int count = passes > 0 ? (passes + gridDim.y - 1) / gridDim.y : 0;
+  if (count == 0) return;
+  int at = blockIdx.x % count;
   const T* src = (const T*)a.qkv + (size_t)row * a.qkv_ld + d0;
   Eight<T> next;
-  const int step = gridDim.y * HPP;
-  int h0 = blockIdx.y * HPP;
-  next.load(src + (size_t)min(h0 + sub, heads - 1) * HD);
+  auto head_of = [&](int i) { return ((int)blockIdx.y + i * (int)gridDim.y) * width; };
+  next.load(src + (size_t)min(head_of(at) + sub, heads - 1) * HD);
   const bool low = d0 < HALF;
   float cs[8], sn[8], qg[8], kg[8];
   {
-    const double pos = (double)(a.pos ? a.pos[row] : slot0 + t);
+    const double pos = (double)(a.pos ? a.pos[row] : pos0);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const double turns = pos * a.turn[d0 % HALF + e];
@@ -150,11 +168,12 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
       kg[e] = a.k_gain ? to_f<T>(((const T*)a.k_gain)[d0 + e]) : 0.f;
     }
   }
-  for (; h0 < heads; h0 += step) {
-    const int h = h0 + sub;
+  for (int i = 0; i < count; ++i) {
+    const int h0 = head_of(at), h = h0 + sub;
+    at = at + 1 == count ? 0 : at + 1;
     float x[8];
     next.floats(x);
-    if (h0 + step < heads) next.load(src + (size_t)min(h0 + step + sub, heads - 1) * HD);
+    if (i + 1 < count) next.load(src + (size_t)min(head_of(at) + sub, heads - 1) * HD);
     if (h0 < a.H + a.c.KVH) {  // uniform: q or k heads
       if (NORM) {
         float ss = 0.f;
@@ -164,7 +183,10 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
         const float sc = 1.0f / sqrtf(ss / (float)HD + a.eps);
         const bool norm = h < a.H ? a.q_gain != nullptr : a.k_gain != nullptr && h < a.H + a.c.KVH;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = norm ? x[e] * sc * (h < a.H ? qg[e] : kg[e]) : x[e];
+        for (int e = 0; e < 8; ++e) {
+          const float gq = qg[e], gk = kg[e];
+          x[e] = norm ? x[e] * sc * (h < a.H ? gq : gk) : x[e];
+        }
       }
       float y[8];
 #pragma unroll
@@ -174,25 +196,30 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
       else if (live && cached && page >= 0 && h < a.H + a.c.KVH)
         store8((T*)a.c.pool + k_off(0, page, a.c.n_blocks, a.c.KVH, HD, h - a.H, t, d0), y);
     }
-    if (h0 + HPP > a.H + a.c.KVH) {  // uniform: v heads
-      const int g0 = h0 - a.H - a.c.KVH;
+    if (rows < 16) {
+      const int g = h - a.H - a.c.KVH;
+      if (g >= 0 && g < a.c.KVH && live && cached && page >= 0) {
+        T* to = (T*)a.c.pool + v_off(0, page, a.c.n_blocks, a.c.KVH, HD, g, t, d0);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) vt[(sub * HD + d0 + e) * kStride + t] = from_f<T>(x[e]);
+        for (int e = 0; e < 8; ++e) to[e * kBlock] = from_f<T>(x[e]);
+      }
+    } else if (h0 + HPP > a.H + a.c.KVH) {  // uniform: v heads of a whole page
+      const int g0 = h0 - a.H - a.c.KVH, end = min(t1, a.c.cap - slot0);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) vt[(l / TPH * HD + d0 + e) * kStride + t] = from_f<T>(x[e]);
       __syncthreads();
-      // tokens of the page that enter it
-      const int t0 = max(len - n - slot0, 0), t1 = min(min(len, a.c.cap) - slot0, 16);
       if (page >= 0) {
         for (int i = threadIdx.x; i < HPP * HD * 16 / kVec; i += 256) {
-          const int d = i * kVec / 16, at = i * kVec % 16, g = g0 + d / HD;
+          const int d = i * kVec / 16, from = i * kVec % 16, g = g0 + d / HD;
           if (g < 0 || g >= a.c.KVH) continue;
-          const T* from = &vt[d * kStride + at];
-          T* to = (T*)a.c.pool + v_off(0, page, a.c.n_blocks, a.c.KVH, HD, g, at, d % HD);
-          if (t0 <= at && at + kVec <= t1) {
-            *(uint4*)to = *(const uint4*)from;
+          const T* v = &vt[d * kStride + from];
+          T* to = (T*)a.c.pool + v_off(0, page, a.c.n_blocks, a.c.KVH, HD, g, from, d % HD);
+          if (t0 <= from && from + kVec <= end) {
+            *(uint4*)to = *(const uint4*)v;
           } else {
 #pragma unroll
             for (int e = 0; e < kVec; ++e)
-              if (at + e >= t0 && at + e < t1) to[e] = from[e];
+              if (from + e >= t0 && from + e < end) to[e] = v[e];
           }
         }
       }
@@ -209,11 +236,12 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
 // (at most 128 terms).
 template <typename T, int HD>
 __global__ __launch_bounds__(64) void paged_means_kernel(MeansArgs a) {
-  const int g = blockIdx.y, seq = blockIdx.z, lane = threadIdx.x;
-  int first, n, all;
+  const int g = blockIdx.y, lane = threadIdx.x;
+  int seq, no, first, n, all;
+  if (!item_of(a.c, blockIdx.x, 1, a.block, 1, seq, no)) return;
   seq_of_wave(a.c, seq, first, n, all);
   const int len = min(all, a.c.cap), old = max(all - n, 0);
-  const int b = old / a.block + blockIdx.x;
+  const int b = old / a.block + no;
   if (b >= len / a.block || b >= a.max_blocks) return;
   float acc[HD / 32][8];
 #pragma unroll
@@ -326,10 +354,10 @@ __global__ __launch_bounds__(256, 4) void paged_score_kernel(SelectArgs a, int p
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int g = blockIdx.y, m = lane & 15, kq = lane >> 4, G = a.H / a.c.KVH;
   int seq, tile, first, n, len;
-  if (!tile_of_item(a.c, blockIdx.x, 1, 16, seq, tile)) return;
+  if (!item_of(a.c, blockIdx.x, 1, 16, 1, seq, tile)) return;
   seq_of_wave(a.c, seq, first, n, len);
   const int r0 = tile * 16;
-  if (tile < 0 || r0 >= n) return;
+  if (r0 >= n) return;
   const int rows = min(16, n - r0);
   // blocks the tile's last row sees (positions past the cap see what the last one does)
   const int last = min(max(len - n + r0 + rows - 1, -1), a.c.cap - 1);
@@ -486,8 +514,9 @@ __global__ __launch_bounds__(256, 8) void paged_choose_kernel(SelectArgs a) {
   for (int i = done + lane; i < a.n_sel; i += 64) out[i] = -1;
 }
 
-// Work-groups an append aims for (8188 rows of 48 heads: 512 52 us, 1024 42, 2048 48,
-// 4096 52: more work out the rotations again, fewer leave loads too few).
+// Work-groups an append aims for, to the nearest count (4 x 2047 rows of 48 heads: 512 62 us,
+// 1024 53, 2048 60; 4 x 1900: 47, 47, 58; 1 x 1000: 14, 15, 20: more work out the rotations again, fewer
+// leave loads too few).
 constexpr int kAppendGroups = 1024;
 
 }  // namespace
@@ -495,7 +524,7 @@ constexpr int kAppendGroups = 1024;
 void launch_paged_append(bool bf16, const AppendArgs& a, hipStream_t s) {
   // passes over heads go to further work-groups where the pages leave compute units idle
   const int pages = a.c.rows / 16 + 2 * a.c.n_seqs, per_pass = 128 / a.hd, heads = a.H + 2 * a.c.KVH;
-  const dim3 grid(pages, std::min((heads + per_pass - 1) / per_pass, (kAppendGroups + pages - 1) / pages));
+  const dim3 grid(pages, std::min((heads + per_pass - 1) / per_pass, std::max(1, (kAppendGroups + pages / 2) / pages)));
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a); };
   const bool norm = a.q_gain || a.k_gain;
   auto by = [&](auto k128, auto n128, auto k64, auto n64) {
@@ -510,7 +539,7 @@ void launch_paged_append(bool bf16, const AppendArgs& a, hipStream_t s) {
 }
 
 void launch_paged_means(bool bf16, const MeansArgs& a, hipStream_t s) {
-  const dim3 grid(a.per_seq, a.c.KVH, a.c.n_seqs);
+  const dim3 grid(a.c.rows / a.block + a.c.n_seqs, a.c.KVH);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64), 0, s, a); };
   if (bf16)
     a.hd == 128 ? go(paged_means_kernel<uint16_t, 128>) : go(paged_means_kernel<uint16_t, 64>);

@@ -372,10 +372,10 @@ __global__ __launch_bounds__(256, (sizeof(T) * HD <= 256 ? 2 : 1)) void paged_st
     seq = seq_of_row(a.c, item / tiles);
     if (seq < 0) return;
   } else {
-    if (!tile_of_item(a.c, item, G, kPagedQueries, seq, tile)) return;
+    if (!item_of(a.c, item, G, kPagedQueries, 1, seq, tile)) return;
   }
   seq_of_wave(a.c, seq, first, n, len);
-  if (tile < 0 || (long long)tile * kPagedQueries >= (long long)n * G) return;
+  if ((long long)tile * kPagedQueries >= (long long)n * G) return;
   Query q;
   int k0, k1;  // the work-group's keys: positions, or places in the row's list
   const int32_t* list = nullptr;
@@ -583,9 +583,9 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a) {
   const int g = blockIdx.x % a.c.KVH, rest = blockIdx.x / a.c.KVH, split = rest % a.n_splits, item = rest / a.n_splits;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, ql = lane & 31, half = lane >> 5;
   int seq, tile, first, n, len;
-  if (!tile_of_item(a.c, item, G, kTileQueries, seq, tile)) return;
+  if (!item_of(a.c, item, G, kTileQueries, 1, seq, tile)) return;
   seq_of_wave(a.c, seq, first, n, len);
-  if (tile < 0 || (long long)tile * kTileQueries >= (long long)n * G) return;
+  if ((long long)tile * kTileQueries >= (long long)n * G) return;
   // the last rows, which see most keys, go first
   tile = (int)(((long long)n * G + kTileQueries - 1) / kTileQueries) - 1 - tile;
   int lo, end;
