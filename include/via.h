@@ -303,7 +303,8 @@ typedef struct {
  *           position.  The pair (i, i + head_dim/2) of a head turns by
  *           pos theta^(-2 i / head_dim).
  *   q_out   [rows][q_ld], written; may be qkv itself with q_ld == qkv_ld (the
- *           queries in place)
+ *           queries in place), and overlap it in no other way (EINVAL is for the
+ *           same address with another length only)
  * Norms and rotations are fp32 (angles fp64), rounded once.  A row without a
  * page gets its query but caches nothing. */
 via_status via_paged_append(const via_paged *c, int32_t slot, const void *qkv, int32_t qkv_ld, int32_t n_heads,

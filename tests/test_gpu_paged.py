@@ -776,3 +776,67 @@ def test_binding_refuses_overlaps_gradients_and_numbers_out_of_range():
     want = step.attend(1, q)
     assert torch.equal(step.attend(1, q, out=qkv[:, 256:]), want)
     assert torch.equal(step.attend(1, q, out=flat[1800:].narrow(0, 0, 768).view(3, 256)), want)
+
+
+def test_thousands_of_sequences():
+    """A search of three steps, with sequences without rows and runs of them."""
+    say("thousands")
+    n_seqs = 4200
+    g = torch.Generator().manual_seed(5)
+    rows = torch.randint(0, 3, (n_seqs,), generator=g)
+    rows[100:400], rows[4100:] = 0, 0
+    lens = (rows + torch.randint(0, 40, (n_seqs,), generator=g)).tolist()
+    b = ref.Batch(F32, 1, 1, 64, rows.tolist(), lens, seed=5, pad=1)
+    step = on_gpu(b)
+    qkv = b.randn(b.T, 3 * 64)
+    q = check_append(b, step, qkv, 10000.0, 1e-5, [None, None], None)
+    b.pool = step.cache.pool.cpu()
+    out, lse = step.attend(b.slot, q, return_lse=True)
+    means = torch.zeros(n_seqs, 1, 2, 64, device="cuda")
+    sel = step.select_blocks(q, step.block_means(b.slot, means, block=32), 2, block=32, n_first=0, n_last=1)
+    some, some_lse = step.attend_blocks(b.slot, q, sel, block=32, return_lse=True)
+    torch.cuda.synchronize()
+    check_attention(b, q.cpu(), out, lse, b.max_kv, 0.125)
+    want, mag = ref.means(b, torch.zeros(n_seqs, 1, 2, 64), 32)
+    assert ((means.double().cpu() - want).abs() <= 7 * 2.0 ** -24 * mag).all()
+    n = b.start[-1]
+    assert torch.equal(sel[:n].cpu(), ref.select(b, q.cpu(), means.cpu(), 2, 32, 0, 1)[:n])
+    check_attention(b, q.cpu(), some, some_lse, 64, 0.125, sel=sel.cpu(), block=32)
+
+
+@pytest.mark.parametrize("dtype,H,KVH,hd", [(BF16, 8, 2, 128), (F32, 2, 1, 64)])
+def test_empty_calls(dtype, H, KVH, hd):
+    """No sequences, no rows, no positions, lengths below 0: outputs of rows with a sequence are those of an
+    empty cache, others stay, and nothing enters the pool."""
+    say("empty", dtype)
+    b = ref.Batch(dtype, H, KVH, hd, [3, 2], [40, 20], seed=1)
+    pool = b.pool.cuda()
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    table = b.table.cuda()
+    for n_seqs, rows, lens, max_kv in ((0, 5, (), 40), (2, 0, (40, 20), 40), (2, 5, (40, 20), 0), (2, 5, (-3, -2 ** 31), 40)):
+        say(n_seqs, rows, lens, max_kv)
+        cache = paged.PagedCache(pool, KVH, hd, table[:n_seqs])
+        step = paged.PagedBatch(cache, ints(*[0, 3, 5][:n_seqs + 1]) if rows else ints(0, 0, 0), ints(*lens), rows, max_kv)
+        qkv = b.randn(rows, (H + 2 * KVH) * hd).to(dtype).cuda()
+        q = torch.full((rows, H, hd), 7.0, dtype=dtype, device="cuda")
+        step.append(1, qkv, H, out=q)
+        live = n_seqs and rows
+        assert not live or (q != 7).any(-1).any(-1).all()
+        means = torch.full((n_seqs, KVH, 2, hd), 7.0, device="cuda")
+        sel = torch.full((rows, KVH, 4), 7, dtype=torch.int32, device="cuda")
+        step.block_means(1, means, block=32)
+        step.select_blocks(q, means, 4, block=32, out=sel)
+        lists = torch.zeros_like(sel)
+        outs = []
+        for f in (lambda o: step.attend(1, q, out=o, return_lse=True), lambda o: step.attend(1, q, window=9, out=o, return_lse=True),
+                  lambda o: step.attend_blocks(1, q, lists, block=32, out=o, return_lse=True)):
+            outs.append(f(torch.full((rows, H, hd), 7.0, dtype=dtype, device="cuda")))
+        torch.cuda.synchronize()
+        assert (means == 7).all()
+        if live:
+            # with max_kv 0 a row has a position still, and sees no block of those that there are
+            assert (sel == -1).all()
+            assert all((o == 0).all() and (z == -math.inf).all() for o, z in outs)
+        else:
+            assert (sel == 7).all() and all((o == 7).all() for o, _ in outs)
+    assert torch.equal(pool.cpu(), b.pool)
