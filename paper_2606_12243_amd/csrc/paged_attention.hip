@@ -561,9 +561,10 @@ __global__ __launch_bounds__(256, (sizeof(T) * HD <= 256 ? 2 : 1)) void paged_st
 // which spares most rescalings of O; weights up to 2^8 lose nothing.
 constexpr int kTileQueries = kPagedTileQueries, kTileKeys = 64;
 
-// 16 bytes a lane from base + voff to LDS at lds + 16 * lane (base, lds wave-uniform)
+// 16 bytes a lane from base + voff to LDS at lds + 16 * lane (base, lds wave-uniform).  A copy into
+// LDS needs a wait state after the write of its m0, which the compiler does not put into inline assembly.
 __device__ __forceinline__ void lds_copy16(const void* base, uint32_t voff, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base), "s"(lds) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base), "s"(lds) : "memory", "m0");
 }
 
 // maximum over the lane and its partner, lane ^ 32
