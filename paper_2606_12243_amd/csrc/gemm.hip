@@ -837,14 +837,16 @@ constexpr int kPfGroupM = 8;
 constexpr int kPfHStride = kPfBN / 2 + 4;  // fp32 per staged h row (padded: no bank conflicts)
 constexpr int kPfLds = kPfStages * kPfStage > kPfBM * kPfHStride * 4 ? kPfStages * kPfStage : kPfBM * kPfHStride * 4;
 
-// 16 bytes per lane from base + voff to LDS at lds + 16 * lane (base wave-uniform)
+// 16 bytes per lane from base + voff to LDS at lds + 16 * lane (base wave-uniform).  A copy into LDS
+// needs a wait state after the write of its m0, which the compiler does not put into inline assembly.
 __device__ __forceinline__ void lds_dma16(const void* base, uint32_t voff, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base), "s"(lds) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base), "s"(lds) : "memory", "m0");
 }
 
 // The same, streamed past the caches.
 __device__ __forceinline__ void lds_dma16_stream(const void* base, uint32_t voff, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(voff), "s"(base), "s"(lds) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(voff), "s"(base), "s"(lds)
+               : "memory", "m0");
 }
 
 template <bool SWIGLU, bool PAIR>

@@ -91,7 +91,7 @@ def test_the_check_sees_an_early_copy():
 
 
 @pytest.mark.skipif(HIPCC is None, reason="needs hipcc")
-@pytest.mark.parametrize("source", ["paged_attention.hip"])
+@pytest.mark.parametrize("source", ["paged_attention.hip", "gemm.hip"])
 def test_no_copy_is_early(source, tmp_path):
     from paper_2606_12243_amd import build
     asm = tmp_path / "out.s"
