@@ -88,13 +88,23 @@ via_status launched(const char* what) {
   return e == hipSuccess ? VIA_OK : fail(VIA_EDEVICE, "%s launch: %s", what, hipGetErrorString(e));
 }
 
-// How the attention's keys are split over work-groups: where the tiles of all
+// How the attention's keys are split over work-groups.  Where the tiles of all
 // K/V heads are fewer than kTargetGroups, each tile's keys are cut into spans of at
-// least kMinSpan.
+// least kMinSpan (of many-row tiles kMinTileSpan), up to kMaxSplits of them.
 constexpr int kTargetGroups = 512;
 constexpr int kMinSpan = 128;
 constexpr int kMinTileSpan = 256;
-constexpr int kMaxSpan = 8192;  // ... and, of several sequences, at most
+// Several sequences are cut into spans of at most kMaxSpan keys besides (or kMaxSplits
+// spans), however many tiles they have: they may differ, and a short batch's long one
+// must not run on its own at the end.  The host knows only their bound, so this stops
+// where its partial results would take more than kPartBytes (of n_splits times rows
+// times heads; splits of the first kind take 34 MB at most) or its launch more
+// work-groups than there can be.  With and without that limit (bf16, 32 heads of 128 on 8): 8 x 1000
+// rows of 2000 keys, bound 131072, 442 and 828 us; 2 x 8192 of 16384, same bound, 3025 and 6791
+// (0 and 4.1 GiB); 8 x 1000 of 32768 4389 and 4369; of 64 x 100 rows one of 60000 keys, the
+// others of 500, 686 and 507.
+constexpr int kMaxSpan = 8192;
+constexpr long long kPartBytes = 256ll << 20;
 struct Split {
   long long n_items;  // tiles a launch covers per K/V head
   int span, n_splits, tile_q, terms;
@@ -128,8 +138,12 @@ Split split_of(const via_paged* c, int n_heads, int window, int n_sel, int block
   const long long groups = std::max<long long>(1, tiles * c->n_kv_heads);
   const long long want = std::min<long long>(std::max<long long>(1, kTargetGroups / groups), kMaxSplits);
   long long span = (keys + want - 1) / want;
-  // sequences may differ: a short batch's long one must not run on its own at the end
-  if (c->n_seqs > 1 && n_sel == 0) span = std::min(span, std::max<long long>(kMaxSpan, (keys + kMaxSplits - 1) / kMaxSplits));
+  if (c->n_seqs > 1 && n_sel == 0) {
+    // (of a split; as many rows times heads as are refused count as that)
+    const long long part = std::clamp((long long)c->rows * n_heads, 1ll, kMaxGroups) * (c->head_dim + 2) * 4;
+    const long long most = std::min({(long long)kMaxSplits, kPartBytes / part, (kMaxGroups - 1) / (s.n_items * c->n_kv_heads)});
+    if (most > 1) span = std::min(span, std::max<long long>(kMaxSpan, (keys + most - 1) / most));
+  }
   span = std::max<long long>(span, s.tile_q == kPagedQueries ? kMinSpan : kMinTileSpan);
   span = (span + 127) / 128 * 128;  // four waves' blocks
   s.span = (int)span;

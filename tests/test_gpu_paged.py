@@ -840,3 +840,21 @@ def test_empty_calls(dtype, H, KVH, hd):
         else:
             assert (sel == 7).all() and all((o == 7).all() for o, _ in outs)
     assert torch.equal(pool.cpu(), b.pool)
+
+
+@pytest.mark.parametrize("rows,lens,max_kv", [([5000, 3600], [9000, 8300], 9000), ([8300, 2], [8300, 20000], 20000)])
+def test_many_rows_of_sequences_too_large_to_split(rows, lens, max_kv):
+    """More partial results than a call asks room for: spans are longer instead.  The last three rows of the
+    first sequence and the last two of the other."""
+    say("too large to split", rows, lens)
+    H, KVH, hd = 64, 2, 128
+    b = ref.Batch(BF16, H, KVH, hd, rows, lens, seed=rows[1])
+    b.max_kv = max_kv
+    step = on_gpu(b)
+    assert via.via_paged_attend_bytes(C.byref(step.c), H, 0) == 0
+    q = torch.randn((b.T, H, hd), dtype=torch.float32, generator=torch.Generator("cuda").manual_seed(1), device="cuda").to(BF16)
+    out, lse = step.attend(b.slot, q, return_lse=True)
+    torch.cuda.synchronize()
+    at = [rows[0] - 3, rows[0] - 2, rows[0] - 1, b.T - 2, b.T - 1]
+    b.rows, b.T, b.start = [3, 2], 5, [0, 3, 5]
+    check_attention(b, q[at].cpu(), out[at], lse[at], max_kv, hd ** -0.5, p_bits=8)

@@ -125,3 +125,26 @@ def test_binding_refuses_what_it_cannot_pass():
         paged.PagedCache(torch.zeros((1, 2, 4, 2, 1024)), 2, 64, table)
     with pytest.raises(ValueError):
         paged.PagedCache(torch.zeros((1, 2, 4, 2, 1024), dtype=torch.float64), 2, 64, table)
+
+
+@pytest.mark.parametrize("rows,n_seqs,max_kv", [(8192, 2, 131072), (32768, 8, 131072), (8188, 4, 1 << 20), (65535, 65535, 400000),
+                                                (4000, 4, 32768), (1 << 17, 3, 1 << 29)])
+def test_many_rows_of_several_sequences_need_no_large_workspace(rows, n_seqs, max_kv):
+    """max_kv is a bound: partial results of every row for each 8192 keys of it would take gigabytes."""
+    d = desc(rows=rows, n_seqs=n_seqs, max_kv=max_kv, table_ld=max_kv // 16 + 1, n_kv_heads=8, head_dim=128)
+    for window in (0, 100000):
+        assert via.via_paged_attend_bytes(C.byref(d), 32, window) <= 256 << 20
+    few = desc(rows=8, n_seqs=2, max_kv=max_kv, table_ld=max_kv // 16 + 1, n_kv_heads=8, head_dim=128)
+    assert via.via_paged_attend_bytes(C.byref(few), 32, 0) > 0  # few rows are still split
+
+
+def test_splits_do_not_outgrow_a_launch():
+    """As many sequences as there may be, over contexts of 2^20: the call wants its workspace, it is not refused."""
+    d = desc(rows=65535, n_seqs=65535, max_kv=1 << 20, table_ld=1 << 16, n_kv_heads=4, head_dim=64)
+    assert 0 < via.via_paged_attend_bytes(C.byref(d), 4, 0) <= 256 << 20
+    assert call("attend", d, ws=None, ws_bytes=0) == via.ENOMEM
+    # sizes that the call refuses: the product of rows, heads and bytes passes 64 bits
+    for rows, heads in ((1 << 27, 2 ** 31 - 4), (1 << 27, 1 << 30), (1 << 25, 1 << 30)):
+        d = desc(rows=rows, n_seqs=2, max_kv=1 << 20, table_ld=1 << 16, n_kv_heads=4, head_dim=128)
+        via.via_paged_attend_bytes(C.byref(d), heads, 0)
+        assert call("attend", d, H=heads, q_ld=2 ** 31 - 8, out_ld=2 ** 31 - 8) == via.EINVAL  # (no row holds them)
