@@ -26,6 +26,7 @@ from __future__ import annotations
 import ctypes as C
 
 import torch
+import torch.autograd.forward_ad as forward_ad
 
 from . import via
 
@@ -43,6 +44,15 @@ def _int32(*values):
             raise ValueError(f"{v} is out of range")
 
 
+def _no_gradient(t, what):
+    """Refuses a tensor that a derivative is asked of, backward or forward: the result would have none."""
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{what} requires a gradient; the operators have none (call them under torch.no_grad)")
+    # (asking a tensor for its tangent costs 1 us: only within a level of forward derivatives)
+    if forward_ad._current_level >= 0 and t.is_floating_point() and forward_ad.unpack_dual(t).tangent is not None:
+        raise ValueError(f"{what} has a forward-mode tangent; the operators have none")
+
+
 class PagedCache:
     """``pool``: contiguous device tensor [n_slots, n_kv_heads, n_blocks, 2, 16 * head_dim]
     (or that many elements flat, with ``n_slots``), fp32 or bf16.  ``table``: int32 [n_seqs,
@@ -51,6 +61,7 @@ class PagedCache:
     def __init__(self, pool, n_kv_heads, head_dim, table, n_slots=None):
         _expect(pool.is_cuda and pool.is_contiguous() and not pool.requires_grad,
                 "the pool must be a contiguous device tensor without a gradient")
+        _no_gradient(pool, "the pool")
         _expect(pool.dtype in _DTYPES, f"a pool of {pool.dtype} (float32 or bfloat16)")
         _expect(n_kv_heads >= 1 and head_dim >= 1, "n_kv_heads and head_dim must be positive")
         n_slots = n_slots if n_slots is not None else (pool.shape[0] if pool.dim() == 5 else 1)
@@ -107,6 +118,7 @@ class PagedBatch:
 
     # ---- arguments
     def _call(self, f, *args):
+        _no_gradient(self.cache.pool, "the pool")
         dev = self.cache.device.index
         stream = torch._C._cuda_getCurrentRawStream(dev)  # (torch.cuda.current_stream builds an object: 2 us)
         if torch.cuda.current_device() == dev:
@@ -122,8 +134,7 @@ class PagedBatch:
         hd, shape, stride = self.cache.head_dim, t.shape, t.stride()
         if t.dtype != self.cache.dtype or t.device != self.cache.device:
             raise ValueError(f"{what} must be {self.cache.dtype} on {self.cache.device}, as the pool is")
-        if t.requires_grad and torch.is_grad_enabled():
-            raise ValueError(f"{what} requires a gradient; the operators have none (call them under torch.no_grad)")
+        _no_gradient(t, what)
         if len(shape) == 3:
             ok = shape[1] == heads and shape[2] == hd and stride[2] == 1 and (heads == 1 or stride[1] == hd)
         else:
@@ -146,8 +157,7 @@ class PagedBatch:
             return None
         if t.dtype != dtype or t.device != self.cache.device or t.shape != shape or not t.is_contiguous():
             raise ValueError(f"{what} must be contiguous {dtype} {list(shape)} on {self.cache.device}")
-        if t.requires_grad and torch.is_grad_enabled():
-            raise ValueError(f"{what} requires a gradient; the operators have none (call them under torch.no_grad)")
+        _no_gradient(t, what)
         return t.data_ptr()
 
     def _apart(self, src, ld, heads, dst, out_ld, out_heads):

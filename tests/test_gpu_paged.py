@@ -858,3 +858,30 @@ def test_many_rows_of_sequences_too_large_to_split(rows, lens, max_kv):
     at = [rows[0] - 3, rows[0] - 2, rows[0] - 1, b.T - 2, b.T - 1]
     b.rows, b.T, b.start = [3, 2], 5, [0, 3, 5]
     check_attention(b, q[at].cpu(), out[at], lse[at], max_kv, hd ** -0.5, p_bits=8)
+
+
+def test_binding_refuses_forward_tangents():
+    import torch.autograd.forward_ad as forward_ad
+    b = ref.Batch(BF16, 4, 2, 64, [3], [40], seed=1)
+    step = on_gpu(b)
+    qkv, gain = torch.zeros(3, 512, dtype=BF16, device="cuda"), torch.ones(64, dtype=BF16, device="cuda")
+    q, means = qkv[:, :256], torch.zeros(1, 2, 2, 64, device="cuda")
+    sel = torch.zeros(3, 2, 4, dtype=torch.int32, device="cuda")
+    with forward_ad.dual_level():
+        dual = lambda t: forward_ad.make_dual(t, torch.ones_like(t))
+        room = torch.zeros(3, 256, dtype=BF16, device="cuda")
+        bad = [
+            lambda: step.append(1, dual(qkv), 4), lambda: step.append(1, qkv, 4, q_gain=dual(gain)),
+            lambda: step.append(1, qkv, 4, k_gain=dual(gain)), lambda: step.attend(1, dual(q)),
+            lambda: step.attend(1, q, out=dual(room)), lambda: step.block_means(1, dual(means), block=32),
+            lambda: step.select_blocks(dual(q), means, 4, block=32), lambda: step.select_blocks(q, dual(means), 4, block=32),
+            lambda: step.attend_blocks(1, dual(q), sel, block=32), lambda: paged.PagedCache(dual(step.cache.pool), 2, 64, step.table),
+        ]
+        for i, f in enumerate(bad):
+            with pytest.raises(ValueError):
+                f()
+                pytest.fail(f"call {i} was not refused")
+        step.append(1, qkv, 4)  # tensors without a tangent are taken
+        step.cache.pool.copy_(dual(step.cache.pool.clone()))
+        with pytest.raises(ValueError):
+            step.attend(1, q)

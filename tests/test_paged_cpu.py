@@ -148,3 +148,21 @@ def test_splits_do_not_outgrow_a_launch():
         d = desc(rows=rows, n_seqs=2, max_kv=1 << 20, table_ld=1 << 16, n_kv_heads=4, head_dim=128)
         via.via_paged_attend_bytes(C.byref(d), heads, 0)
         assert call("attend", d, H=heads, q_ld=2 ** 31 - 8, out_ld=2 ** 31 - 8) == via.EINVAL  # (no row holds them)
+
+
+def test_no_derivative_is_dropped():
+    """Tensors that a backward or forward derivative is asked of are refused."""
+    torch = pytest.importorskip("torch")
+    import torch.autograd.forward_ad as forward_ad
+    from paper_2606_12243_amd import paged
+    x = torch.zeros(4)
+    paged._no_gradient(x, "x")
+    with pytest.raises(ValueError, match="x requires a gradient"):
+        paged._no_gradient(torch.zeros(4, requires_grad=True), "x")
+    with forward_ad.dual_level():
+        paged._no_gradient(x, "x")
+        paged._no_gradient(torch.zeros(4, dtype=torch.int32), "x")
+        dual = forward_ad.make_dual(x, torch.ones(4))
+        for t in (dual, dual[:2], dual.view(2, 2)):
+            with torch.no_grad(), pytest.raises(ValueError, match="x has a forward-mode tangent"):
+                paged._no_gradient(t, "x")
