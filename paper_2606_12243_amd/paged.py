@@ -110,6 +110,7 @@ class PagedBatch:
         # (a table that is part of a wider one: no more than its own columns)
         _int32(rows, cache.n_blocks, cache.n_slots, self.table.stride(0))
         self.rows, self.max_kv, self.n_seqs = int(rows), min(int(max_kv), self.table.shape[1] * via.BLOCK), n
+        _int32(self.max_kv)
         self.c = via.Paged(cache.pool.data_ptr(), _DTYPES[cache.dtype], cache.n_slots, cache.n_blocks, cache.n_kv_heads,
                            cache.head_dim, self.table.data_ptr(), max(1, self.table.stride(0)), n, row_start.data_ptr(),
                            kv_len.data_ptr(), self.rows, self.max_kv)

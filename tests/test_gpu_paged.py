@@ -885,3 +885,14 @@ def test_binding_refuses_forward_tangents():
         step.cache.pool.copy_(dual(step.cache.pool.clone()))
         with pytest.raises(ValueError):
             step.attend(1, q)
+
+
+def test_binding_refuses_bounds_past_32_bits():
+    b = ref.Batch(BF16, 4, 2, 64, [3], [40], seed=1)
+    step = on_gpu(b)
+    q = torch.ones(3, 4, 64, dtype=BF16, device="cuda")
+    for max_kv in (-(1 << 32), -(1 << 31) - 1):  # (32 bits of the first: 0, an empty cache)
+        with pytest.raises(ValueError):
+            paged.PagedBatch(step.cache, step.row_start, step.kv_len, 3, max_kv)
+    most = paged.PagedBatch(step.cache, step.row_start, step.kv_len, 3, 1 << 40)  # the table's columns bound it
+    assert torch.equal(most.attend(1, q), step.attend(1, q))
