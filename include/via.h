@@ -281,9 +281,11 @@ via_status via_dimr_cost(const float *q_logits, const float *p_logits, int32_t r
  * no-op.  Row arrays (q, out, ...) are row-major of `dtype` with a row length
  * in elements; they and their rows are 16-byte aligned (EINVAL).  n_heads is a
  * multiple of n_kv_heads, query head h reading K/V head h / (n_heads /
- * n_kv_heads).  head_dim is 64 or 128, at most 65535 sequences and
- * 2^27 rows, and rows times heads below 2^24 for the attention and the choice of
- * blocks (EUNSUPPORTED). */
+ * n_kv_heads).  head_dim is 64 or 128, at most 65535 sequences, 65535 K/V heads
+ * and 2^27 rows; for the attention rows times heads are below 2^24, and so are sequences times
+ * K/V heads and a 32nd of rows times heads together; for the choice of blocks rows times K/V heads
+ * are (EUNSUPPORTED).  The attention's kernels and splits follow the average rows of
+ * a sequence and max_kv, so a row's last bits may change with its batch. */
 typedef struct {
   void *pool;
   int32_t dtype, n_slots, n_blocks, n_kv_heads, head_dim;
@@ -319,13 +321,13 @@ via_status via_paged_append(const via_paged *c, int32_t slot, const void *qkv, i
  *             [rows]: a row sees the positions before the batch's, and position
  *             kv_len - n + o (o < min(n, VIA_MAX_TREE_ROWS)) iff bit o of its mask
  *             is set (a token tree; give no window, EINVAL).
- *   out       [rows][out_ld], written; a row that sees nothing gets zeros.  May be q
- *             itself with out_ld == q_ld, and overlap it in no other way (EINVAL is
+ *   out       [rows][out_ld], written; a row that sees nothing, or only scores of
+ *             -infinity, gets zeros.  May be q itself with out_ld == q_ld, and overlap it in no other way (EINVAL is
  *             for the same address with another length only)
  *   lse       fp32 [rows][n_heads] or NULL: log of the sum of exp(scale q K^T), -inf
- *             for a row that sees nothing
+ *             for such a row
  *   workspace device, 256-byte aligned, >= via_paged_attend_bytes (ENOMEM; may be
- *             NULL where that is 0)
+ *             NULL where that is 0; never more than 256 MiB)
  * scale > 0.  A key that a row does not see adds nothing to it, whatever its page
  * holds.  Scores, softmax and sums are fp32; a bf16 call of 128 queries (rows times
  * heads of a K/V head) a sequence or more, on average, rounds the softmax's weights to
@@ -353,7 +355,8 @@ via_status via_paged_block_means(const via_paged *c, int32_t slot, int32_t block
  *   means  as via_paged_block_means keeps them; max_blocks must cover max_kv
  *   sel    device [rows][n_kv_heads][n_sel], written: ascending blocks, then -1
  *          where the row sees fewer
- *   workspace device, 256-byte aligned, >= via_paged_select_bytes (ENOMEM)
+ *   workspace device, 256-byte aligned, >= via_paged_select_bytes (ENOMEM): the scores, 8 bytes
+ *             for each row, K/V head and block that max_kv allows
  * n_first + n_last <= n_sel.  The pool and the table are given as for the other
  * calls and not read. */
 size_t via_paged_select_bytes(const via_paged *c, int32_t block);
@@ -364,7 +367,10 @@ via_status via_paged_select(const via_paged *c, const void *q, int32_t q_ld, int
 /* via_paged_attend over chosen blocks: row r sees, under K/V head g, the
  * positions up to its own of the blocks sel[r][g][0 .. n_sel) (device int32, any
  * order; a block listed twice counts twice, an entry that is negative or past
- * the row's own block is passed over).  The other arguments are
+ * the row's own block is passed over).  There is no row mask: the rows of a token tree
+ * would see those of their siblings that lie before them.  Every row reads its blocks
+ * for itself, so it is for few rows over a long context; from about 64 rows of a sequence on
+ * via_paged_attend over 32000 keys takes less time.  The other arguments are
  * via_paged_attend's. */
 size_t via_paged_attend_blocks_bytes(const via_paged *c, int32_t n_heads, int32_t block, int32_t n_sel);
 via_status via_paged_attend_blocks(const via_paged *c, int32_t slot, const void *q, int32_t q_ld, int32_t n_heads,

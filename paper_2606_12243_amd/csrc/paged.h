@@ -18,7 +18,7 @@ struct PagedRef {
   const int32_t* row_start;  // [n_seqs + 1]
   const int32_t* kv_len;     // [n_seqs]
   int rows;                  // rows of the row arrays
-  int cap;                   // cache positions a call looks at: min(max_kv, table_ld * kBlock)
+  int cap;                   // cache positions a call looks at: min(max_kv, table_ld * kBlock, 2^30)
   int pages;                 // table entries that these are in
 };
 
@@ -80,7 +80,7 @@ struct SelectArgs {
   int max_blocks, block, n_first, n_last, n_sel;
   int32_t* sel;      // [rows][KVH][n_sel]
   uint64_t* scores;  // workspace [rows][KVH][nb]: sortable scores
-  int nb;            // blocks a row may see: min(max_blocks, ceil(cap / block))
+  int nb;            // blocks a row may see: ceil(cap / block), at most max_blocks
 };
 
 void launch_paged_append(bool bf16, const AppendArgs& a, hipStream_t s);

@@ -896,3 +896,35 @@ def test_binding_refuses_bounds_past_32_bits():
             paged.PagedBatch(step.cache, step.row_start, step.kv_len, 3, max_kv)
     most = paged.PagedBatch(step.cache, step.row_start, step.kv_len, 3, 1 << 40)  # the table's columns bound it
     assert torch.equal(most.attend(1, q), step.attend(1, q))
+
+
+@pytest.mark.parametrize("dtype,H,KVH,hd,rows,lens", [(BF16, 8, 2, 128, [3, 2], [40, 700]), (F32, 2, 1, 64, [3, 2], [40, 700]),
+                                                      (BF16, 8, 2, 64, [60, 60], [60, 700])])
+def test_scores_of_minus_infinity(dtype, H, KVH, hd, rows, lens):
+    """Keys of -infinity have no weight; a row that sees no others gets zeros, as one that sees none."""
+    say("minus infinity", dtype, H, KVH, hd, rows, lens)
+    b = ref.Batch(dtype, H, KVH, hd, rows, lens, seed=lens[1])
+    clean = b.pool.clone()
+    k = b.pool[b.slot][:, :, 0].view(KVH, b.n_blocks, hd // 8, 16, 8)
+    for pos in range(lens[0]):
+        k[:, b.page(0, pos), 0, pos % 16, 0] = -math.inf
+    for pos in range(lens[1] - 3):
+        k[:, b.page(1, pos), 0, pos % 16, 0] = -math.inf
+    q = b.randn(b.T, H, hd).to(dtype)
+    q[:, :, 0] = 1.0
+    out, lse = on_gpu(b).attend(b.slot, q.cuda(), return_lse=True)
+    torch.cuda.synchronize()
+    n = rows[0]
+    assert (out[:n] == 0).all() and (lse[:n] == -math.inf).all()
+    blind = n + rows[1] - 3 if rows[1] > 3 else n  # rows of the other that see only such keys
+    assert (out[n:blind] == 0).all() and (lse[n:blind] == -math.inf).all()
+    # the others see the last keys alone, as a window would have it
+    b.pool = clean
+    at = list(range(blind, b.T))
+    last = ref.Batch(dtype, H, KVH, hd, rows, lens, seed=lens[1])
+    last.rows, last.T, last.start, last.pool = [0, len(at)], len(at), [0, 0, len(at)], clean
+    for i, t in enumerate(at):
+        last.rows, last.T, last.start, last.lens = [0, 1], 1, [0, 0, 1], [lens[0], lens[1] - len(at) + 1 + i]
+        window = last.lens[1] - (lens[1] - 3)
+        check_attention(last, q[t:t + 1], out[t:t + 1], lse[t:t + 1], 3, hd ** -0.5, p_bits=weight_bits(b),
+                        window=window)

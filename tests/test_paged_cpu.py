@@ -166,3 +166,13 @@ def test_no_derivative_is_dropped():
         for t in (dual, dual[:2], dual.view(2, 2)):
             with torch.no_grad(), pytest.raises(ValueError, match="x has a forward-mode tangent"):
                 paged._no_gradient(t, "x")
+
+
+def test_sequences_times_heads_have_an_end():
+    for op in ("attend", "blocks"):
+        d = desc(rows=1 << 17, n_seqs=65535, n_kv_heads=256, head_dim=64)
+        assert call(op, d, H=256, q_ld=1 << 14, out_ld=1 << 14) == via.EUNSUPPORTED, op
+    d = desc(rows=65535, n_seqs=65535, n_kv_heads=257, head_dim=64)
+    assert call("attend", d, H=257, q_ld=1 << 15, out_ld=1 << 15) == via.EUNSUPPORTED
+    d = desc(rows=1, n_seqs=65535, n_kv_heads=257, head_dim=64)  # one row, as many sequences
+    assert call("attend", d, H=257, q_ld=1 << 15, out_ld=1 << 15) == via.EUNSUPPORTED
