@@ -928,3 +928,19 @@ def test_scores_of_minus_infinity(dtype, H, KVH, hd, rows, lens):
         window = last.lens[1] - (lens[1] - 3)
         check_attention(last, q[t:t + 1], out[t:t + 1], lse[t:t + 1], 3, hd ** -0.5, p_bits=weight_bits(b),
                         window=window)
+
+
+def test_spans_longer_than_usual():
+    """Partial results limited to fewer, longer spans: two of 15104 keys here instead of four."""
+    say("longer spans")
+    H, KVH, hd = 64, 2, 128
+    rows, lens = [2500, 200], [30000, 9000]
+    b = ref.Batch(BF16, H, KVH, hd, rows, lens, seed=4)
+    step = on_gpu(b)
+    assert via.via_paged_attend_bytes(C.byref(step.c), H, 0) == 2 * b.T * H * (hd + 2) * 4
+    q = torch.randn((b.T, H, hd), dtype=torch.float32, generator=torch.Generator("cuda").manual_seed(2), device="cuda").to(BF16)
+    out, lse = step.attend(b.slot, q, return_lse=True)
+    torch.cuda.synchronize()
+    at = [rows[0] - 2, rows[0] - 1, b.T - 2, b.T - 1]
+    b.rows, b.T, b.start = [2, 2], 4, [0, 2, 4]
+    check_attention(b, q[at].cpu(), out[at], lse[at], b.max_kv, hd ** -0.5, p_bits=8)
